@@ -397,6 +397,43 @@ int gnnpre_lc_selftest_wait_timeout(const float* hop, int64_t n, int64_t feat_di
                                     uint32_t polls, void* stream);
 
 /*
+ * Learned tables (no counterpart in the paper: X_0 of a graph whose nodes have categories instead of features, and the rows
+ * that gnnpre_lc_first_layer gathers when a table is trained).
+ *
+ *   gnnpre_embedding_lookup   out[i][c] = scale * table[ids[i]][c],                    i < count, c < dim
+ *   gnnpre_embedding_grad     d_table[v][c] = scale * sum over { i : ids[i] = v } of d_out[i][c]   (plus the old value
+ *                             with `accumulate`), v < n
+ *
+ *   table, out     DEVICE, row-major, both of `dtype` (GNNPRE_F32, GNNPRE_BF16 or GNNPRE_F16), leading dimensions ldt, ldo
+ *   ids            DEVICE int32 (GNNPRE_I32) or int64 (GNNPRE_I64) [count].  NOT validated: an id outside [0, n) is
+ *                  padding, whose row reads as zeros and adds nothing to the gradient, whatever d_out holds there
+ *   d_out          DEVICE, of `dtype`, [count, dim], leading dimension ldd
+ *   d_table        DEVICE, [n, dim], leading dimension ldt, of `dtype` or GNNPRE_F32.  Without `accumulate` every row is
+ *                  written (rows nobody asked for become zero); with it only rows that some id asks for are touched
+ *   workspace      DEVICE, 256-byte aligned, gnnpre_embedding_grad_workspace(n, dim, count) bytes (which returns a negative
+ *                  status for sizes that the call refuses).  In use until the call's work completes: one per stream, and
+ *                  one per captured graph that may run beside others
+ * 1 <= n < 2^31, 1 <= dim <= 2^20, 0 <= count < 2^31; leading dimensions >= dim; nothing that is written may overlap what is read
+ * (else INVALID_ARG).  Pointers need the alignment of their elements only (else ALIGN); rows that start on 16-byte boundaries
+ * are the fast case.  Columns beyond dim are neither read nor written.
+ * Arithmetic: products and sums in fp32, rounded once to the output's type.  The gradient adds the rows of one id in the order
+ * of their positions, in pieces of a length that depends on `count` alone, and the pieces in a fixed order: results are
+ * bitwise reproducible.
+ * The work is enqueued on `stream` and the call returns without synchronising; nothing is allocated.
+ */
+#define GNNPRE_F32 0
+#define GNNPRE_BF16 1
+#define GNNPRE_F16 2
+#define GNNPRE_I32 0
+#define GNNPRE_I64 1
+int gnnpre_embedding_lookup(const void* table, int64_t n, int64_t dim, int64_t ldt, int32_t dtype, const void* ids,
+                            int32_t ids_type, int64_t count, float scale, void* out, int64_t ldo, void* stream);
+int64_t gnnpre_embedding_grad_workspace(int64_t n, int64_t dim, int64_t count);
+int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dtype, const void* ids, int32_t ids_type, int64_t count,
+                          int64_t n, int64_t dim, float scale, int32_t accumulate, void* d_table, int64_t ldt,
+                          int32_t table_dtype, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * Measurement aid (no counterpart in the paper): the fetches of ONE hop and nothing else.  Walks the plan's
  * segments exactly as gnnpre_propagate's segment kernels do - same column tiles, same index stream, same
  * fetch path (128-bit loads into registers, or bulk copies into shared memory, by row width) - adds every

@@ -249,3 +249,26 @@ def weighted_hop_sum(op: int, eps: float, rowptr, colidx, X, gamma) -> np.ndarra
     _c().orc_weighted_hop_sum(op, float(eps), n, _ptr(rowptr), _ptr(colidx), X.shape[1], _ptr(X), ldx,
                               gamma.shape[0] - 1, _ptr(gamma), _ptr(Z))
     return Z
+
+
+def embedding_lookup(table, ids, scale: float) -> np.ndarray:
+    """scale * table[ids] in fp64; an id outside the table gives a row of zeros."""
+    table, ids = np.asarray(table, dtype=np.float64), np.asarray(ids, dtype=np.int64)
+    out = np.zeros((ids.size, table.shape[1]))
+    known = (ids >= 0) & (ids < table.shape[0])
+    out[known] = scale * table[ids[known]]
+    return out
+
+
+def embedding_grad(d_out, ids, num_rows: int, scale: float, want_abs: bool = False):
+    """Row v: scale * sum of the rows of d_out whose id is v, in fp64 (want_abs: also the sum of the terms' absolute values, and
+    how many there are)."""
+    d_out, ids = np.asarray(d_out, dtype=np.float64), np.asarray(ids, dtype=np.int64)
+    known = np.flatnonzero((ids >= 0) & (ids < num_rows))
+    out = np.zeros((num_rows, d_out.shape[1]))
+    np.add.at(out, ids[known], scale * d_out[known])
+    if not want_abs:
+        return out
+    size = np.zeros_like(out)
+    np.add.at(size, ids[known], abs(scale) * np.abs(d_out[known]))
+    return out, size, np.bincount(ids[known], minlength=num_rows)

@@ -94,6 +94,10 @@ def _load() -> ctypes.CDLL:
                                               ctypes.POINTER(ctypes.c_float), p, i64, p]
     lib.gnnpre_lc_first_layer.argtypes = [ctypes.POINTER(ctypes.c_void_p), i32, i64, i64, i64, p, i64, p, i64, i64,
                                           ctypes.c_uint64, i32, p, i64, i64, p, p]
+    lib.gnnpre_embedding_lookup.argtypes = [p, i64, i64, i64, i32, p, i32, i64, ctypes.c_float, p, i64, p]
+    lib.gnnpre_embedding_grad_workspace.argtypes = [i64, i64, i64]
+    lib.gnnpre_embedding_grad_workspace.restype = i64
+    lib.gnnpre_embedding_grad.argtypes = [p, i64, i32, p, i32, i64, i64, i64, ctypes.c_float, i32, p, i64, i32, p, i64, p]
     lib.gnnpre_normalize.argtypes = [p, p, i32, p]
     lib.gnnpre_solve_normalisation_blocks.argtypes = [i64] * 8 + [ctypes.POINTER(i64)]
     lib.gnnpre_selftest_wait_timeout.argtypes = [p, ctypes.c_uint32, p]
@@ -358,6 +362,84 @@ def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, 
     return out
 
 
+GNNPRE_F32, GNNPRE_BF16, GNNPRE_F16 = 0, 1, 2
+GNNPRE_I32, GNNPRE_I64 = 0, 1
+_DTYPES = {torch.float32: GNNPRE_F32, torch.bfloat16: GNNPRE_BF16, torch.float16: GNNPRE_F16}
+_ID_TYPES = {torch.int32: GNNPRE_I32, torch.int64: GNNPRE_I64}
+
+
+def _on_current_device(*tensors) -> None:
+    """The library launches on the current device's stream: operands of another device are refused."""
+    current = torch.cuda.current_device()
+    for t in tensors:
+        assert t.is_cuda and t.get_device() == current
+
+
+def _rows(t: torch.Tensor) -> int:
+    """Leading dimension of a row-major matrix (a matrix of one row or none may have any)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _workspace(given: torch.Tensor | None, size: int, where: str, device) -> torch.Tensor:
+    if size < 0:
+        raise GnnpreError(size, where)
+    if given is None:
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    assert given.dtype is torch.uint8 and given.is_contiguous() and given.numel() >= size
+    return given
+
+
+def gnnpre_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, out: torch.Tensor | None = None,
+                            stream=None) -> torch.Tensor:
+    """scale * table[ids] ([N, D]); an id outside the table (padding) gives a row of zeros.
+
+    table: device fp32, bf16 or fp16 [V, D] with stride(1) == 1; ids: device int32 or int64 [N]; out: of table's type."""
+    assert table.dim() == 2 and table.dtype in _DTYPES and ids.dim() == 1 and ids.dtype in _ID_TYPES and ids.is_contiguous()
+    (V, D), N = table.shape, ids.shape[0]
+    assert table.stride(1) == 1 or D == 1
+    if out is None:
+        out = torch.empty((N, D), dtype=table.dtype, device=table.device)
+    assert out.dtype is table.dtype and out.shape == (N, D) and (out.stride(1) == 1 or D == 1)
+    _on_current_device(table, ids, out)
+    _check(_lib.gnnpre_embedding_lookup(table.data_ptr(), V, D, _rows(table), _DTYPES[table.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype],
+                                        N, scale, out.data_ptr(), _rows(out), _stream_ptr(stream)), "gnnpre_embedding_lookup")
+    return out
+
+
+def gnnpre_embedding_grad_workspace(num_rows: int, dim: int, count: int) -> int:
+    """Bytes of workspace that gnnpre_embedding_grad needs for `count` ids into a [num_rows, dim] table."""
+    size = _lib.gnnpre_embedding_grad_workspace(num_rows, dim, count)
+    if size < 0:
+        raise GnnpreError(size, "gnnpre_embedding_grad_workspace")
+    return size
+
+
+def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int, *, scale: float = 1.0, out: torch.Tensor | None = None,
+                          accumulate: bool = False, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Gradient of gnnpre_embedding_lookup in its table: row v is scale * (sum of the rows of d_out whose id is v), [num_rows, D].
+
+    d_out: device fp32, bf16 or fp16 [N, D]; out: of d_out's type or fp32 (the default).  With accumulate=True it is added to
+    out (rows that no id asks for stay untouched).  workspace: uint8 tensor of gnnpre_embedding_grad_workspace bytes, for callers
+    that keep one; otherwise one is taken from torch's allocator on the current stream."""
+    assert d_out.dim() == 2 and d_out.dtype in _DTYPES and ids.dim() == 1 and ids.dtype in _ID_TYPES and ids.is_contiguous()
+    N, D = d_out.shape
+    assert ids.shape[0] == N and (d_out.stride(1) == 1 or D == 1)
+    assert out is not None or not accumulate
+    if out is None:
+        out = torch.empty((num_rows, D), dtype=torch.float32, device=d_out.device)
+    assert out.dtype in (d_out.dtype, torch.float32) and out.shape == (num_rows, D) and (out.stride(1) == 1 or D == 1)
+    _on_current_device(d_out, ids, out)
+    size = _lib.gnnpre_embedding_grad_workspace(num_rows, D, N)
+    room = _workspace(workspace, size, "gnnpre_embedding_grad", d_out.device)
+    _on_current_device(room)
+    _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), _rows(d_out), _DTYPES[d_out.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype], N,
+                                      num_rows, D, scale, int(accumulate), out.data_ptr(), _rows(out), _DTYPES[out.dtype],
+                                      room.data_ptr(), room.numel(), _stream_ptr(stream)), "gnnpre_embedding_grad")
+    if workspace is None and stream is not None:
+        room.record_stream(stream)  # allocated on the current stream, used on another
+    return out
+
+
 def gnnpre_normalize(plan: Plan, out: torch.Tensor | None = None, *, host: bool = False, stream=None) -> torch.Tensor:
     """fp32 value of every edge of the support (order of gnnpre_plan_support), on the device or in host memory."""
     m = plan.nnz_tilde
@@ -447,6 +529,7 @@ def gnnpre_status_string(status: int) -> str:
 def exported_symbols():
     return ["gnnpre_degrees", "gnnpre_build_plan", "gnnpre_plan_info", "gnnpre_plan_block", "gnnpre_plan_scales",
             "gnnpre_plan_support", "gnnpre_plan_hop_order", "gnnpre_propagate", "gnnpre_propagate_weighted", "gnnpre_hop_static", "gnnpre_lc_first_layer", "gnnpre_lc_selftest_wait_timeout", "gnnpre_normalize",
+            "gnnpre_embedding_lookup", "gnnpre_embedding_grad_workspace", "gnnpre_embedding_grad",
             "gnnpre_solve_normalisation_blocks", "gnnpre_selftest_wait_timeout", "gnnpre_selftest_wait_timeout_async",
             "gnnpre_plan_status", "gnnpre_inject_alloc_failure", "gnnpre_gather_ceiling", "gnnpre_describe_panels", "gnnpre_plan_destroy", "gnnpre_release_cached_memory", "gnnpre_solve_budget",
             "gnnpre_status_string", "gnnpre_last_cuda_error"]
