@@ -434,6 +434,44 @@ int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dtype, const v
                           int32_t table_dtype, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * An update orthogonalised by Newton-Schulz products (no counterpart in the paper: the step that turns the gradient of a weight
+ * such as gnnpre_lc_first_layer's into an update whose singular values are all of one size).  For each of `batch` matrices
+ *
+ *     X_0 = G / (||G||_F + eps),    A = X X^T,    X <- (a I + b A + c A^2) X   `steps` times,    out = scale * X
+ *
+ * with (a, b, c) = coeffs; on G's transpose where G has more rows than columns, which gives the same matrix.
+ *
+ *   G, out      DEVICE, row-major [rows, cols] of `dtype` (GNNPRE_F32, GNNPRE_BF16, GNNPRE_F16), leading dimensions ldg, ldo;
+ *               matrix k begins at G + k * g_stride, out + k * o_stride (elements).  out may be G
+ *   coeffs      HOST, three floats.  They must keep the singular values, which start in [0, 1], below 16 in every step, and
+ *               |a + b t + c t^2| below 1024 there (else INVALID_ARG)
+ *   workspace   DEVICE, 256-byte aligned, gnnpre_orthogonalize_workspace(batch, rows, cols, steps) bytes (which returns a
+ *               negative status for sizes that the call refuses).  In use until the call's work completes: one per stream, and
+ *               one per captured graph that may run beside others
+ *   error_flag  DEVICE int32 or NULL; set to 1 by a kernel if one of its bounded waits ran out (the results are then invalid).
+ *               The caller clears and reads it.
+ * 1 <= rows, cols <= 65536, 0 <= batch <= 16384, 1 <= steps <= 64, eps >= 0 and finite; ldg, ldo >= cols, matrices of out apart
+ * (else INVALID_ARG).  Pointers need the alignment of their elements (else ALIGN).
+ * Arithmetic: the norm in fp64; operands of the products carry 22 bits (two fp16 numbers each, scaled by a power of two that the
+ * coefficients fix), products summed in fp32, one rounding to the output's type.  A matrix of zeros stays one (with eps = 0 it
+ * becomes NaN); a NaN or an infinity anywhere in a matrix makes that matrix NaN.
+ * The work is enqueued on `stream` and the call returns without synchronising; nothing is allocated.
+ */
+int64_t gnnpre_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int32_t steps);
+int gnnpre_orthogonalize(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_stride, int64_t batch, int32_t dtype,
+                         int32_t steps, const float* coeffs, float eps, float scale, void* out, int64_t ldo, int64_t o_stride,
+                         void* workspace, int64_t workspace_bytes, int32_t* error_flag, void* stream);
+
+/*
+ * Failure-detection self-test of gnnpre_orthogonalize's products, as gnnpre_lc_selftest_wait_timeout: one step on an fp32
+ * [rows, cols] matrix in which nobody hears of the copies that have landed, so that every bounded wait gives up after `polls`
+ * polls (1..100000).  Synchronises; returns GNNPRE_ERR_TIMEOUT when the error word was raised (the expected outcome).  `out`
+ * receives nothing meaningful; workspace as for gnnpre_orthogonalize(1, rows, cols, 1).
+ */
+int gnnpre_orthogonalize_selftest_wait_timeout(const float* G, int64_t rows, int64_t cols, float* out, void* workspace,
+                                               int64_t workspace_bytes, int32_t* error_flag, uint32_t polls, void* stream);
+
+/*
  * Measurement aid (no counterpart in the paper): the fetches of ONE hop and nothing else.  Walks the plan's
  * segments exactly as gnnpre_propagate's segment kernels do - same column tiles, same index stream, same
  * fetch path (128-bit loads into registers, or bulk copies into shared memory, by row width) - adds every

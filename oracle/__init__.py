@@ -272,3 +272,15 @@ def embedding_grad(d_out, ids, num_rows: int, scale: float, want_abs: bool = Fal
     size = np.zeros_like(out)
     np.add.at(size, ids[known], abs(scale) * np.abs(d_out[known]))
     return out, size, np.bincount(ids[known], minlength=num_rows)
+
+
+def orthogonalize(G, steps: int, coeffs, eps: float, scale: float) -> np.ndarray:
+    """scale * X after `steps` steps X <- (a I + b A + c A^2) X, A = X X^T, from X = G / (||G||_F + eps), in fp64; [rows, cols] or a
+    stack of them."""
+    a, b, c = coeffs
+    X = np.asarray(G, dtype=np.float64)
+    X = X / (np.sqrt((X ** 2).sum(axis=(-2, -1), keepdims=True)) + eps)
+    for _ in range(steps):
+        A = X @ np.swapaxes(X, -1, -2)
+        X = a * X + b * (A @ X) + c * (A @ (A @ X))
+    return scale * X

@@ -98,6 +98,11 @@ def _load() -> ctypes.CDLL:
     lib.gnnpre_embedding_grad_workspace.argtypes = [i64, i64, i64]
     lib.gnnpre_embedding_grad_workspace.restype = i64
     lib.gnnpre_embedding_grad.argtypes = [p, i64, i32, p, i32, i64, i64, i64, ctypes.c_float, i32, p, i64, i32, p, i64, p]
+    lib.gnnpre_orthogonalize_workspace.argtypes = [i64, i64, i64, i32]
+    lib.gnnpre_orthogonalize_workspace.restype = i64
+    lib.gnnpre_orthogonalize.argtypes = [p, i64, i64, i64, i64, i64, i32, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float,
+                                         ctypes.c_float, p, i64, i64, p, i64, p, p]
+    lib.gnnpre_orthogonalize_selftest_wait_timeout.argtypes = [p, i64, i64, p, p, i64, p, ctypes.c_uint32, p]
     lib.gnnpre_normalize.argtypes = [p, p, i32, p]
     lib.gnnpre_solve_normalisation_blocks.argtypes = [i64] * 8 + [ctypes.POINTER(i64)]
     lib.gnnpre_selftest_wait_timeout.argtypes = [p, ctypes.c_uint32, p]
@@ -430,7 +435,8 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
     assert out.dtype in (d_out.dtype, torch.float32) and out.shape == (num_rows, D) and (out.stride(1) == 1 or D == 1)
     _on_current_device(d_out, ids, out)
     size = _lib.gnnpre_embedding_grad_workspace(num_rows, D, N)
-    room = _workspace(workspace, size, "gnnpre_embedding_grad", d_out.device)
+    room = _workspace(workspace, size, "gnnpre_embedding_grad",
+            "gnnpre_orthogonalize_workspace", "gnnpre_orthogonalize", "gnnpre_orthogonalize_selftest_wait_timeout", d_out.device)
     _on_current_device(room)
     _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), _rows(d_out), _DTYPES[d_out.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype], N,
                                       num_rows, D, scale, int(accumulate), out.data_ptr(), _rows(out), _DTYPES[out.dtype],
@@ -438,6 +444,64 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
     if workspace is None and stream is not None:
         room.record_stream(stream)  # allocated on the current stream, used on another
     return out
+
+
+def gnnpre_orthogonalize_workspace(batch: int, rows: int, cols: int, steps: int) -> int:
+    """Bytes of workspace that gnnpre_orthogonalize needs for `batch` matrices of [rows, cols]."""
+    size = _lib.gnnpre_orthogonalize_workspace(batch, rows, cols, steps)
+    if size < 0:
+        raise GnnpreError(size, "gnnpre_orthogonalize_workspace")
+    return size
+
+
+def gnnpre_orthogonalize(G: torch.Tensor, *, steps: int = 5, coeffs=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, scale: float = 1.0,
+                         out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, check: bool = True,
+                         stream=None) -> torch.Tensor:
+    """scale * X after `steps` steps X <- (a I + b A + c A^2) X, A = X X^T, from X = G / (||G||_F + eps): an update with its singular
+    values brought to about one size.
+
+    G: device fp32, bf16 or fp16 [rows, cols] or [batch, rows, cols] with stride 1 along the columns; out: of its type and shape, may
+    be G.  workspace: uint8 tensor of gnnpre_orthogonalize_workspace bytes, for callers that keep one.  With check=True the call
+    synchronises and raises if a device-side wait ran out."""
+    assert G.dim() in (2, 3) and G.dtype in _DTYPES
+    if out is None:
+        out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+    assert out.dtype is G.dtype and out.shape == G.shape
+    a, o = (t if t.dim() == 3 else t.unsqueeze(0) for t in (G, out))
+    n, rows, cols = a.shape
+    assert (a.stride(2) == 1 or cols == 1) and (o.stride(2) == 1 or cols == 1)
+    _on_current_device(G, out)
+    size = _lib.gnnpre_orthogonalize_workspace(n, rows, cols, steps)
+    room = _workspace(workspace, size, "gnnpre_orthogonalize", G.device)
+    _on_current_device(room)
+    flag = torch.zeros(1, dtype=torch.int32, device=G.device) if check else None
+    if check and stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())  # the flag is cleared on the current one
+    ld = [max(t.stride(1), cols) if rows == 1 else t.stride(1) for t in (a, o)]
+    _check(_lib.gnnpre_orthogonalize(a.data_ptr(), rows, cols, ld[0], a.stride(0), n, _DTYPES[G.dtype], steps,
+                                     (ctypes.c_float * 3)(*[float(c) for c in coeffs]), eps, scale, o.data_ptr(), ld[1], o.stride(0),
+                                     room.data_ptr(), room.numel(), flag.data_ptr() if check else None, _stream_ptr(stream)),
+           "gnnpre_orthogonalize")
+    if workspace is None and stream is not None:
+        room.record_stream(stream)
+    if check:
+        if stream is not None:
+            stream.synchronize()
+        if int(flag.item()) != 0:
+            raise GnnpreError(-8, "gnnpre_orthogonalize")
+    return out
+
+
+def gnnpre_orthogonalize_selftest_wait_timeout(G: torch.Tensor, polls: int = 200, stream=None) -> int:
+    """Status of products whose waits are made to run out (expected: -8, GNNPRE_ERR_TIMEOUT)."""
+    rows, cols = G.shape
+    assert G.dtype is torch.float32 and G.is_contiguous()
+    out = torch.empty_like(G)
+    room = torch.empty(gnnpre_orthogonalize_workspace(1, rows, cols, 1), dtype=torch.uint8, device=G.device)
+    flag = torch.zeros(1, dtype=torch.int32, device=G.device)
+    _on_current_device(G)
+    return int(_lib.gnnpre_orthogonalize_selftest_wait_timeout(G.data_ptr(), rows, cols, out.data_ptr(), room.data_ptr(), room.numel(),
+                                                               flag.data_ptr(), polls, _stream_ptr(stream)))
 
 
 def gnnpre_normalize(plan: Plan, out: torch.Tensor | None = None, *, host: bool = False, stream=None) -> torch.Tensor:

@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["plan.cu", "propagate.cu", "stream.cu", "noalloc.cu", "normalize.cu", "lc_layer.cu",
-           "embedding.cu", "api.cu"]
+           "embedding.cu", "orthogonalize.cu", "api.cu"]
 LIB = os.path.join(HERE, "lib", "libgnnpre.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -19,7 +19,7 @@ def _inputs():
     hdr = [os.path.join(HERE, "csrc", "gnnpre_internal.cuh"), os.path.join(HERE, "csrc", "segments_tma.cuh"),
            os.path.join(HERE, "csrc", "segments.cuh"), os.path.join(HERE, "csrc", "segments_common.cuh"), os.path.join(HERE, "csrc", "fixups.cuh"), os.path.join(HERE, "csrc", "ceiling.cuh"),
            os.path.join(HERE, "csrc", "segment_rules.h"), os.path.join(HERE, "csrc", "lc_rules.h"),
-           os.path.join(HERE, "csrc", "dense.cuh"),
+           os.path.join(HERE, "csrc", "dense.cuh"), os.path.join(HERE, "csrc", "tensor_core.cuh"),
            os.path.join(ROOT, "include", "gnnpre.h")]
     return src, hdr
 

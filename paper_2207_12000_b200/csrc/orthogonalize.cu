@@ -1,0 +1,693 @@
+// An update orthogonalised by Newton-Schulz products:
+//
+//   X_0 = G / (||G||_F + eps),   A = X X^T,   X <- (a I + b A + c A^2) X   `steps` times,   out = scale X
+//
+// on the smaller side of G (X is [r, n] with r <= n, G or its transpose).  Everything is matrix products, on the tensor cores.
+//
+// Numbers.  ||X_0||_F <= 1, so every singular value starts in [0, 1] and the polynomial's coefficients bound all that follows
+// (computed on the host; coefficients under which the iterates may grow without such a bound are refused).  A matrix with a known
+// bound is held as 2^e times itself in two fp16 numbers, high and low part, e chosen so that the bound just fits: 22 significant
+// bits, and an absolute error far below that of fp32 sums of the same size.  A product takes three tensor-core products (high x
+// high, high x low, low x high) into one fp32 accumulator; what is dropped is below 2^-22 of the operands.  fp16 carries
+// 11 bits where tf32 carries as many at half the rate and bf16 carries 8: one fp16 product in place of the three would lose the
+// small singular values, which a step multiplies by a (3.4) and with them the rounding errors of the large ones.
+//
+// Order of the products.  The polynomials of a few steps commute and are polynomials of the first A, so they can be multiplied
+// together before X: with P = aI + bA + cA^2, X <- P X makes A <- P A P.  A segment of g steps is
+//     A = X X^T;   g times { P = aI + bA + cA^2;  T = A P;  A = T P;  Q = Q P };   X = Q X
+// (the last step needs no T and A, the first no Q).  The r x r products are symmetric: only the lower tiles are computed.  That
+// saves work on matrices that are not square, at the price of an error of A that grows by a^2 per step where an A formed anew has
+// none of it: [256, 128] with six strong directions is off by 1.8e-6 in steps by themselves (as plain fp32 is) and by 2.0e-4 in
+// segments of three.  So segments have three steps at most for bf16 outputs (one rounding: 1.7e-3), two for fp16, one for fp32.
+//
+// Layout.  Operands are stored as the tensor core reads them: blocks of 128 rows x 64 columns of K in the 128-byte swizzle, the
+// high parts' 16 KB and then the low parts', so an operand tile is one contiguous copy and needs no tensor map.
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "dense.cuh"
+#include "tensor_core.cuh"
+
+namespace gnnpre {
+namespace {
+
+constexpr int kBlockRows = 128, kBlockCols = 64;
+constexpr int kHalfBytes = kBlockRows * kBlockCols * 2;  // one part of a block
+constexpr int kBlockBytes = 2 * kHalfBytes;
+constexpr int kPipeBytes = 192 * 1024;
+constexpr int kSumWarps = 8, kCopyWarp = 8, kMmaWarp = 9;
+constexpr int kProductThreads = 320;
+constexpr int kSliceChunks = 1;                          // chunks of 64 of K in one accumulator
+constexpr int kMaxSteps = 64;
+constexpr float kMostSpectral = 16.f;    // bound of X under which coefficients are accepted
+constexpr int64_t kMaxSide = 1 << 16;
+
+// A split matrix [rows, cols], both padded: block (rb, kb) of a batch entry.
+struct Split {
+    unsigned char* p;
+    int64_t batch_bytes;
+    int32_t kblocks;
+    __device__ __forceinline__ unsigned char* block(int64_t batch, int rb, int kb) const {
+        return p + batch * batch_bytes + ((int64_t)rb * kblocks + kb) * kBlockBytes;
+    }
+};
+
+// Byte of element (row, col) of a block's part.
+__device__ __forceinline__ uint32_t block_byte(int row, int col) {
+    return (uint32_t)(row * 128 + ((((col >> 3) ^ (row & 7)) & 7) << 4) + (col & 7) * 2);
+}
+
+// v as 2^e v in two fp16 numbers, eight of them at a time.
+__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 hh = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        const float2 back = __half22float2(hh);
+        const __half2 ll = __floats2half2_rn(v[2 * i] - back.x, v[2 * i + 1] - back.y);
+        h[i] = *reinterpret_cast<const uint32_t*>(&hh);
+        l[i] = *reinterpret_cast<const uint32_t*>(&ll);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// ------------------------------------------------------------------------------------------------ norm and first split
+
+struct Source {
+    const void* g;
+    int64_t ldg, batch_stride;
+    int32_t rows, cols;      // of G
+    int32_t dtype;
+    int32_t tall;            // rows > cols: X is G's transpose
+    double eps;
+    double* partial;         // [batch][kNormBlocks]
+    float factor;            // 2^e of X
+    Split x, xt;
+};
+
+constexpr int kNormBlocks = 64;
+constexpr int kNormThreads = 256;
+
+__device__ __forceinline__ float source_at(const Source& s, int64_t batch, int64_t i, int64_t j) {
+    const int64_t at = batch * s.batch_stride + i * s.ldg + j;
+    if (s.dtype == GNNPRE_F32) return static_cast<const float*>(s.g)[at];
+    if (s.dtype == GNNPRE_BF16) return to_f32(static_cast<const __nv_bfloat16*>(s.g)[at]);
+    return to_f32(static_cast<const __half*>(s.g)[at]);
+}
+
+// Squares in 64 bits: neither tiny nor huge updates lose their norm.
+__global__ void __launch_bounds__(kNormThreads) k_ns_norm(const Source s) {
+    __shared__ double room[kNormThreads / 32];
+    double sum = 0;
+    for (int64_t i = blockIdx.x; i < s.rows; i += gridDim.x)
+        for (int64_t j = threadIdx.x; j < s.cols; j += kNormThreads) {
+            const double v = source_at(s, blockIdx.y, i, j);
+            sum += v * v;
+        }
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormThreads / 32; ++w) sum += room[w];
+        s.partial[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+    }
+}
+
+// X and its transpose, split: a CTA takes [64, 64] of X.
+__global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t norm_blocks) {
+    wait_previous_kernel();
+    __shared__ float tile[64][65];
+    __shared__ double inverse;
+    const int64_t batch = blockIdx.z;
+    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;  // of X
+    if (threadIdx.x == 0) {
+        double sum = 0;
+        for (int b = 0; b < norm_blocks; ++b) sum += s.partial[batch * kNormBlocks + b];
+        inverse = 1.0 / (sqrt(sum) + s.eps);
+    }
+    __syncthreads();
+    const double scale = inverse * (double)s.factor;
+    const int fast = threadIdx.x & 63;
+    for (int slow = threadIdx.x >> 6; slow < 64; slow += 4) {
+        const int gi = (s.tall ? j0 : i0) + slow, gj = (s.tall ? i0 : j0) + fast;  // neighbouring threads, neighbouring elements of G
+        const float v = gi < s.rows && gj < s.cols ? (float)((double)source_at(s, batch, gi, gj) * scale) : 0.f;
+        if (s.tall) tile[fast][slow] = v;
+        else tile[slow][fast] = v;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 64 * 8; c += 256) {
+        const int row = c >> 3, chunk = c & 7;
+        float v[8];
+        uint4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[row][8 * chunk + e];
+        split8(v, hi, lo);
+        unsigned char* d = s.x.block(batch, (i0 + row) / kBlockRows, j0 / kBlockCols) + block_byte((i0 + row) % kBlockRows, 8 * chunk);
+        *reinterpret_cast<uint4*>(d) = hi;
+        *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[8 * chunk + e][row];
+        split8(v, hi, lo);
+        d = s.xt.block(batch, (j0 + row) / kBlockRows, i0 / kBlockCols) + block_byte((j0 + row) % kBlockRows, 8 * chunk);
+        *reinterpret_cast<uint4*>(d) = hi;
+        *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ products
+
+// D = alpha * (A B^T) + beta * C + diag * I over the stored (scaled) numbers.
+struct Job {
+    Split a, b, c, d, dt;
+    float alpha, beta, diag;
+    int32_t k_chunks;
+    int32_t has_c, write_t;  // write_t: D's transpose as well
+};
+
+struct Product {
+    Job job[2];
+    int32_t jobs;
+    int32_t tiles_n;     // of BN columns
+    int32_t symmetric;   // D = D^T: only tiles on and below the diagonal, the others by their transposes
+    int32_t* error;
+    uint32_t spin_limit;
+    int32_t drop;        // self-test: the copies' bytes are not announced
+    // the last product writes the caller's matrix instead
+    void* out;           // nullptr: it does not
+    int64_t ldo, out_batch;
+    int32_t out_dtype, out_rows, out_cols;
+    float out_factor;
+};
+
+// One tile of 128 x BN per CTA.  Warps 0-7 add up and store: warps w and w + 4 share the accumulator's lanes 32 (w & 3) .. and
+// take a half of the columns each; warp 8 copies, warp 9 multiplies.
+//
+// The tensor core cuts, not rounds, a sum that it adds a product to: over K = 4000 in one accumulator the sums of squares in A
+// came out 1e-5 too small (750 additions, half of 2^-23 each).  So an accumulator takes one chunk only, its small terms first, so
+// that four cuts count; two take turns, and their sums are added up in registers, rounded to nearest, while the next ones form.
+template <int BN>
+__global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_constant__ Product a) {
+    constexpr uint32_t kBBytes = BN * 128;                  // one part of B's chunk
+    constexpr uint32_t kStage = kBlockBytes + 2 * kBBytes;
+    constexpr int kStages = kPipeBytes / kStage;
+    constexpr int kCols = BN / 2;                           // of a thread
+    extern __shared__ unsigned char ns_smem[];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 5];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    volatile int* abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (tc_smem(ns_smem) + 1023u) & ~1023u;
+    unsigned char* const base_p = ns_smem + (base - tc_smem(ns_smem));
+    const uint32_t bar0 = tc_smem(&bars[0]);
+    auto full = [&](int s) { return bar0 + 8u * s; };
+    auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+    auto acc_full = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
+    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
+    const uint32_t drained = bar0 + 8u * (2 * kStages + 4);
+    const Job& job = a.job[blockIdx.z % a.jobs];
+    const int64_t batch = blockIdx.z / a.jobs;
+    int bi, bj;  // tile row (of 128), tile column (of BN)
+    if (a.symmetric) {
+        bi = (int)((sqrtf(8.f * blockIdx.x + 1.f) - 1.f) * 0.5f);
+        while ((bi + 1) * (bi + 2) / 2 <= (int)blockIdx.x) ++bi;
+        while (bi * (bi + 1) / 2 > (int)blockIdx.x) --bi;
+        bj = blockIdx.x - bi * (bi + 1) / 2;
+    } else {
+        bi = blockIdx.x / a.tiles_n;
+        bj = blockIdx.x % a.tiles_n;
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc_bar_init(full(s), 1 + (a.drop ? 1 : 0));
+            tc_bar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc_bar_init(acc_full(b), 1);
+            tc_bar_init(acc_empty(b), kSumWarps);
+        }
+        tc_bar_init(drained, 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), 2 * BN);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    wait_previous_kernel();
+
+    const int slices = (job.k_chunks + kSliceChunks - 1) / kSliceChunks;
+    float sum[kCols];
+    bool ok = true;
+    if (warp < kSumWarps) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
+        const uint32_t taddr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (warp >> 2) * kCols;
+        for (int i = 0; i < slices; ++i) {
+            ok = tc_wait_warp(acc_full(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, a.error, a.spin_limit);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int part = 0; part < kCols / 32; ++part) {
+                uint32_t v[32];
+                tc_load32(taddr + (uint32_t)(i & 1) * BN + 32 * part, v);
+                tc_load_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) sum[32 * part + j] += __uint_as_float(v[j]);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc_bar_arrive(acc_empty(i & 1));
+        }
+    } else if (warp == kCopyWarp) {
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            uint32_t ph = 0;
+            const int rows0 = bj * BN % kBlockRows, rb = bj * BN / kBlockRows;
+            for (int kc = 0; kc < job.k_chunks; ++kc, ++issued) {
+                ok = tc_wait(empty(s), ph ^ 1u, abort_flag, a.error, a.spin_limit);
+                if (!ok) break;
+                const uint32_t to = base + (uint32_t)s * kStage;
+                const unsigned char* b = job.b.block(batch, rb, kc);
+                tc_bar_expect(full(s), kStage);
+                tc_bulk_load(to, job.a.block(batch, bi, kc), kBlockBytes, full(s));
+                if (BN == kBlockRows) {
+                    tc_bulk_load(to + kBlockBytes, b, kBlockBytes, full(s));
+                } else {
+                    tc_bulk_load(to + kBlockBytes, b + rows0 * 128, kBBytes, full(s));
+                    tc_bulk_load(to + kBlockBytes + kBBytes, b + kHalfBytes + rows0 * 128, kBBytes, full(s));
+                }
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+            // Every copy has landed before this CTA's memory is used again or given up.  (A self-test's barriers wait for one
+            // more arrival: theirs is made up for once the waits have run out.)
+            if (a.drop) {
+                for (uint32_t i = 0; i < 4 * a.spin_limit && !*abort_flag; ++i) __nanosleep(kTcSuspendNs);
+                *abort_flag = 1;
+            }
+            for (int t = 0; t < min(issued, kStages); ++t) {
+                const int uses = (issued - t + kStages - 1) / kStages;
+                if (a.drop) tc_bar_arrive(full(t));
+                for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+                    if (tc_bar_test(full(t), (uint32_t)(uses - 1) & 1u)) break;
+            }
+        }
+        __syncwarp();
+    } else if (warp == kMmaWarp) {
+        const uint32_t instr = tc_instr(kBlockRows, BN, false);
+        int s = 0;
+        uint32_t ph = 0;
+        for (int i = 0, kc = 0; i < slices && ok; ++i) {
+            ok = tc_wait_warp(acc_empty(i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
+            for (int first = kc; ok && kc < min(first + kSliceChunks, job.k_chunks); ++kc) {
+                ok = tc_wait_warp(full(s), ph, abort_flag, a.error, a.spin_limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = base + (uint32_t)s * kStage, d = tmem + (uint32_t)(i & 1) * BN;
+                const uint64_t ah = tc_desc_k(at), al = tc_desc_k(at + kHalfBytes), bh = tc_desc_k(at + kBlockBytes),
+                               bl = tc_desc_k(at + kBlockBytes + kBBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) {  // the small terms first
+                    tc_mma(d, al + 2 * j, bh + 2 * j, instr, kc != first || j != 0);
+                    tc_mma(d, ah + 2 * j, bl + 2 * j, instr, 1u);
+                }
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(d, ah + 2 * j, bh + 2 * j, instr, 1u);
+                tc_commit(empty(s));
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+            if (ok) tc_commit(acc_full(i & 1));
+        }
+        // tensor memory is freed, and shared memory used again, when the tensor core is done
+        tc_commit(drained);
+        for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+            if (tc_bar_test(drained, 0)) break;
+        __syncwarp();
+    }
+    ok = __syncthreads_and(ok);
+    const int q = warp & 3, half = (warp >> 2) & 1, row = 32 * q + lane;
+    if (ok && a.out) {
+        float* line = reinterpret_cast<float*>(base_p) + warp * (32 * 33);
+        if (warp < kSumWarps)
+#pragma unroll
+            for (int part = 0; part < kCols / 32; ++part) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[32 * part + j] * a.out_factor;
+                __syncwarp();
+                const int col = bj * BN + half * kCols + 32 * part + lane;
+                if (col < a.out_cols)
+                    for (int r = 0; r < 32; ++r) {
+                        const int64_t i = (int64_t)bi * kBlockRows + 32 * q + r;
+                        if (i >= a.out_rows) break;
+                        const int64_t at = batch * a.out_batch + i * a.ldo + col;
+                        const float o = line[r * 33 + lane];
+                        if (a.out_dtype == GNNPRE_F32) static_cast<float*>(a.out)[at] = o;
+                        else if (a.out_dtype == GNNPRE_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(o);
+                        else static_cast<__half*>(a.out)[at] = __float2half_rn(o);
+                    }
+                __syncwarp();
+            }
+    } else if (ok) {
+        // D's blocks of 64 columns lie behind one another in shared memory, then its transpose's blocks of 64 columns (a row of
+        // those is a column of the tile); both go out as they lie.
+        const bool transposed = job.write_t || (a.symmetric && bi != bj);
+        unsigned char* const tile_t = base_p + BN / kBlockCols * kBlockBytes;
+        if (warp < kSumWarps)
+#pragma unroll
+            for (int part = 0; part < kCols / 32; ++part) {
+                const int c0 = half * kCols + 32 * part;
+                const int col0 = bj * BN + c0;  // of D
+                const int diag = bi * kBlockRows + row - col0;  // the column of these 32 that lies on the diagonal
+                const unsigned char* c = job.has_c ? job.c.block(batch, bi, col0 / kBlockCols) : nullptr;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = job.alpha * sum[32 * part + 8 * j + e];
+                    if (job.has_c) {
+                        const uint4 ch = *reinterpret_cast<const uint4*>(c + block_byte(row, col0 % kBlockCols + 8 * j));
+                        const uint4 cl = *reinterpret_cast<const uint4*>(c + kHalfBytes + block_byte(row, col0 % kBlockCols + 8 * j));
+                        const __half2* h = reinterpret_cast<const __half2*>(&ch);
+                        const __half2* l = reinterpret_cast<const __half2*>(&cl);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 fh = __half22float2(h[e]), fl = __half22float2(l[e]);
+                            o[2 * e] = fmaf(job.beta, fh.x + fl.x, o[2 * e]);
+                            o[2 * e + 1] = fmaf(job.beta, fh.y + fl.y, o[2 * e + 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (8 * j + e == diag) o[e] += job.diag;
+                    uint4 hi, lo;
+                    split8(o, hi, lo);
+                    unsigned char* d = base_p + c0 / kBlockCols * kBlockBytes + block_byte(row, c0 % kBlockCols + 8 * j);
+                    *reinterpret_cast<uint4*>(d) = hi;
+                    *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+                    if (transposed) {
+                        const __half* h = reinterpret_cast<const __half*>(&hi);
+                        const __half* l = reinterpret_cast<const __half*>(&lo);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            unsigned char* t = tile_t + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
+                            *reinterpret_cast<__half*>(t) = h[e];
+                            *reinterpret_cast<__half*>(t + kBBytes) = l[e];
+                        }
+                    }
+                }
+            }
+        tc_fence_async();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int b = 0; b < BN / kBlockCols; ++b)
+                tc_bulk_store(job.d.block(batch, bi, bj * (BN / kBlockCols) + b), base + b * kBlockBytes, kBlockBytes);
+            if (transposed) {
+                const Split& to = job.write_t ? job.dt : job.d;
+                const int rows0 = bj * BN % kBlockRows;
+                const uint32_t from = base + BN / kBlockCols * kBlockBytes;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    unsigned char* t = to.block(batch, bj * BN / kBlockRows, 2 * bi + b) + rows0 * 128;
+                    tc_bulk_store(t, from + b * 2 * kBBytes, kBBytes);
+                    tc_bulk_store(t + kHalfBytes, from + b * 2 * kBBytes + kBBytes, kBBytes);
+                }
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+    }
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tc_free(tmem, 2 * BN);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+struct Bounds {
+    double x[kMaxSteps + 1];  // largest singular value before step k
+    double p[kMaxSteps];      // largest eigenvalue of |P| in step k
+};
+
+// How large the polynomials can make the singular values, which start in [0, 1]; false: beyond kMostSpectral.
+bool bounds_of(const float* coeffs, int32_t steps, Bounds* out) {
+    const double a = coeffs[0], b = coeffs[1], c = coeffs[2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    double r = 1.0;
+    for (int32_t k = 0; k < steps; ++k) {
+        r *= 1.0 + 1e-4;  // what rounding adds
+        out->x[k] = r;
+        const double u1 = r * r;
+        const auto p = [&](double u) { return std::fabs(a + b * u + c * u * u); };
+        const auto x = [&](double u) { return std::sqrt(u) * p(u); };
+        double mp = std::max(p(0), p(u1)), mx = x(u1);
+        const auto inside = [&](double u, bool slope) {
+            if (!(u > 0 && u < u1)) return;
+            if (slope) mx = std::max(mx, x(u));
+            else mp = std::max(mp, p(u));
+        };
+        if (c != 0) inside(-b / (2 * c), false);
+        // d/ds (a s + b s^3 + c s^5) = a + 3 b u + 5 c u^2,  u = s^2
+        if (c != 0) {
+            const double d = 9 * b * b - 20 * a * c;
+            if (d >= 0) {
+                inside((-3 * b + std::sqrt(d)) / (10 * c), true);
+                inside((-3 * b - std::sqrt(d)) / (10 * c), true);
+            }
+        } else if (b != 0) {
+            inside(-a / (3 * b), true);
+        }
+        out->p[k] = mp;
+        r = mx;
+        if (!(r <= kMostSpectral) || !(mp <= 1024.0)) return false;
+    }
+    out->x[steps] = r;
+    return true;
+}
+
+// 2^e with which a matrix of this bound fits fp16 with room to spare.
+int exponent_for(double bound) { return std::max(-8, std::min(14, (int)std::floor(std::log2(32768.0 / std::max(bound, 1e-6))))); }
+
+struct NsShape {
+    int64_t r, n, rp, np, batch;
+    int32_t segment;  // steps at most between two X
+    int64_t side, square;  // bytes of one split [rp, np], [rp, rp]
+    int64_t xt[2], x, a, t, p, q[2], partial, total;
+};
+
+// Steps of a segment at most (see above).
+int32_t most_segment_steps(int32_t dtype) { return dtype == GNNPRE_BF16 ? 3 : dtype == GNNPRE_F16 ? 2 : 1; }
+
+NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32_t most) {
+    NsShape s{};
+    s.batch = batch;
+    s.r = std::min(rows, cols);
+    s.n = std::max(rows, cols);
+    s.rp = (s.r + 127) / 128 * 128;
+    s.np = (s.n + 127) / 128 * 128;
+    // multiplications per step of a segment of g steps, in units of r^2: n + 2 n for its ends, (4 g - 3) r between
+    const auto cost = [&](int g) { return (3.0 * s.np + (4.0 * g - 3.0) * s.rp) / g; };
+    s.segment = 1;
+    for (int g = 2; g <= std::min(most, steps); ++g)
+        if (cost(g) < 0.99 * cost(s.segment)) s.segment = g;
+    s.side = s.rp * s.np * 4;
+    s.square = s.rp * s.rp * 4;
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += (bytes * batch + 1023) / 1024 * 1024;
+        return here;
+    };
+    s.x = take(s.side);
+    s.xt[0] = take(s.side);
+    s.xt[1] = steps > s.segment ? take(s.side) : s.xt[0];
+    s.a = take(s.square);
+    s.p = take(s.square);
+    s.q[0] = s.segment > 1 ? take(s.square) : s.p;
+    s.q[1] = s.segment > 1 ? take(s.square) : s.p;
+    s.t = s.segment > 1 ? take(s.square) : s.p;
+    s.partial = take((int64_t)sizeof(double) * kNormBlocks);
+    s.total = at;
+    return s;
+}
+
+struct NsSelfTest {
+    int32_t drop;
+    uint32_t polls;
+};
+
+template <int BN>
+int launch_product_n(const Product& a, int64_t tiles_m, int64_t batch, cudaStream_t st) {
+    constexpr int kSmem = kPipeBytes + 1024;
+    static std::atomic<bool> opted_in[kMaxDevices];
+    int dev = 0;
+    GNNPRE_CUDA(cudaGetDevice(&dev));
+    if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
+        GNNPRE_CUDA(cudaFuncSetAttribute(k_ns_product<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
+    }
+    const int64_t tiles = a.symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * a.tiles_n;
+    return launch_after(k_ns_product<BN>, dim3((unsigned)tiles, 1, (unsigned)(batch * a.jobs)), kProductThreads, kSmem, true, st, a);
+}
+
+// D has rows x cols elements.
+int launch_product(Product& a, int64_t rows, int64_t cols, int64_t batch, bool symmetric, int sms, cudaStream_t st) {
+    const int64_t tiles_m = rows / 128;
+    // Tiles of 128 x 64 while they fit the machine; symmetric products need square ones to leave any out.
+    const bool narrow = tiles_m * (cols / 64) * batch * a.jobs <= sms;
+    a.symmetric = symmetric && !narrow && tiles_m > 1;
+    a.tiles_n = (int32_t)(narrow ? cols / 64 : cols / 128);
+    return narrow ? launch_product_n<64>(a, tiles_m, batch, st) : launch_product_n<128>(a, tiles_m, batch, st);
+}
+
+int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_stride, int64_t batch, int32_t dtype, int32_t steps,
+              const float* coeffs, float eps, float scale, void* out, int64_t ldo, int64_t o_stride, void* workspace,
+              int64_t workspace_bytes, int32_t* error_flag, void* stream, const NsSelfTest* test = nullptr) {
+    if (!is_dtype(dtype) || rows < 1 || cols < 1 || rows > kMaxSide || cols > kMaxSide || batch < 0 || batch > 16384) return GNNPRE_ERR_INVALID_ARG;
+    if (steps < 1 || steps > kMaxSteps || !coeffs || !(eps >= 0.f) || !std::isfinite(eps)) return GNNPRE_ERR_INVALID_ARG;
+    Bounds bound;
+    if (!bounds_of(coeffs, steps, &bound)) return GNNPRE_ERR_INVALID_ARG;
+    if (batch == 0) return GNNPRE_OK;
+    if (!G || !out || !workspace || ldg < cols || ldo < cols) return GNNPRE_ERR_INVALID_ARG;
+    if (batch > 1 && (g_stride < 0 || o_stride < (rows - 1) * ldo + cols)) return GNNPRE_ERR_INVALID_ARG;
+    const int64_t es = dtype_bytes(dtype);
+    if (reinterpret_cast<uintptr_t>(G) % es || reinterpret_cast<uintptr_t>(out) % es || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return GNNPRE_ERR_ALIGN;
+    const NsShape s = ns_shape(batch, rows, cols, steps, most_segment_steps(dtype));
+    if (workspace_bytes < s.total) return GNNPRE_ERR_INVALID_ARG;
+    const int64_t span_g = (batch - 1) * g_stride + (rows - 1) * ldg + cols, span_o = (batch - 1) * o_stride + (rows - 1) * ldo + cols;
+    if (arrays_overlap(workspace, 1, s.total, 1, 1, G, 1, span_g, 1, es) || arrays_overlap(workspace, 1, s.total, 1, 1, out, 1, span_o, 1, es))
+        return GNNPRE_ERR_INVALID_ARG;
+    int sms = 0;
+    GNNPRE_TRY(device_sms(&sms));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    unsigned char* w = static_cast<unsigned char*>(workspace);
+    const auto side = [&](int64_t at) { return Split{w + at, s.side, (int32_t)(s.np / 64)}; };
+    const auto side_t = [&](int64_t at) { return Split{w + at, s.side, (int32_t)(s.rp / 64)}; };
+    const auto square = [&](int64_t at) { return Split{w + at, s.square, (int32_t)(s.rp / 64)}; };
+
+    int ex = exponent_for(bound.x[0]);
+    Source src{G, ldg, g_stride, (int32_t)rows, (int32_t)cols, dtype, rows > cols, (double)eps, reinterpret_cast<double*>(w + s.partial),
+               (float)std::ldexp(1.0, ex), side(s.x), side_t(s.xt[0])};
+    const int norm_blocks = (int)std::min<int64_t>(kNormBlocks, rows);
+    k_ns_norm<<<dim3((unsigned)norm_blocks, (unsigned)batch), kNormThreads, 0, st>>>(src);
+    GNNPRE_CUDA(cudaGetLastError());
+    GNNPRE_TRY(launch_after(k_ns_split, dim3((unsigned)(s.np / 64), (unsigned)(s.rp / 64), (unsigned)batch), 256, 0, true, st, src, norm_blocks));
+
+    Product base{};
+    base.error = error_flag;
+    base.spin_limit = test ? test->polls : kTcSpinLimit;
+    base.drop = test ? test->drop : 0;
+    base.jobs = 1;
+    const int32_t k_r = (int32_t)((s.r + 63) / 64), k_n = (int32_t)((s.n + 63) / 64);
+    int xt = 0;
+    for (int32_t k = 0; k < steps;) {
+        const int32_t g = std::min(s.segment, steps - k);
+        int ea = exponent_for(bound.x[k] * bound.x[k]);
+        Product m = base;
+        m.job[0] = Job{side(s.x), side(s.x), {}, square(s.a), {}, (float)std::ldexp(1.0, ea - 2 * ex), 0.f, 0.f, k_n, 0, 0};
+        GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+        int eq = 0, q = 0;
+        double q_bound = 1;
+        for (int32_t j = 0; j < g; ++j) {
+            // P = a I + b A + c A A
+            const int ep = exponent_for(bound.p[k + j]);
+            const Split p = square(j == 0 ? s.q[0] : s.p);
+            m = base;
+            m.job[0] = Job{square(s.a), square(s.a), square(s.a), p, {}, (float)std::ldexp((double)coeffs[2], ep - 2 * ea),
+                           (float)std::ldexp((double)coeffs[1], ep - ea), (float)std::ldexp((double)coeffs[0], ep), k_r, 1, 0};
+            GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+            q_bound *= bound.p[k + j];
+            const int eq_new = j == 0 ? ep : exponent_for(q_bound);
+            const Job more = {square(s.q[q]), p, {}, square(s.q[q ^ 1]), {}, (float)std::ldexp(1.0, eq_new - eq - ep), 0.f, 0.f, k_r, 0, 0};
+            m = base;
+            if (j + 1 < g) {
+                // T = A P, then the next A = T P beside Q = Q P
+                const int et = exponent_for(bound.x[k + j] * bound.x[k + j] * bound.p[k + j]), ea_new = exponent_for(bound.x[k + j + 1] * bound.x[k + j + 1]);
+                m.job[0] = Job{square(s.a), p, {}, square(s.t), {}, (float)std::ldexp(1.0, et - ea - ep), 0.f, 0.f, k_r, 0, 0};
+                GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+                m = base;
+                m.job[0] = Job{square(s.t), p, {}, square(s.a), {}, (float)std::ldexp(1.0, ea_new - et - ep), 0.f, 0.f, k_r, 0, 0};
+                if (j > 0) {
+                    m.job[1] = more;
+                    m.jobs = 2;
+                }
+                GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+                ea = ea_new;
+            } else if (j > 0) {
+                m.job[0] = more;
+                GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+            }
+            if (j > 0) q ^= 1;
+            eq = eq_new;
+        }
+        k += g;
+        m = base;
+        if (k < steps) {
+            const int ex_new = exponent_for(bound.x[k]);
+            m.job[0] = Job{square(s.q[q]), side_t(s.xt[xt]), {}, side(s.x), side_t(s.xt[xt ^ 1]), (float)std::ldexp(1.0, ex_new - eq - ex), 0.f, 0.f, k_r, 0, 1};
+            GNNPRE_TRY(launch_product(m, s.rp, s.np, batch, false, sms, st));
+            ex = ex_new;
+            xt ^= 1;
+            continue;
+        }
+        m.out = out;
+        m.ldo = ldo;
+        m.out_batch = o_stride;
+        m.out_dtype = dtype;
+        m.out_rows = (int32_t)rows;
+        m.out_cols = (int32_t)cols;
+        m.out_factor = (float)std::ldexp((double)scale, -eq - ex);
+        // Q is symmetric: the transpose of Q X is X^T Q
+        const bool tall = rows > cols;
+        m.job[0] = Job{tall ? side_t(s.xt[xt]) : square(s.q[q]), tall ? square(s.q[q]) : side_t(s.xt[xt]), {}, {}, {}, 1.f, 0.f, 0.f, k_r, 0, 0};
+        GNNPRE_TRY(launch_product(m, tall ? s.np : s.rp, tall ? s.rp : s.np, batch, false, sms, st));
+    }
+    return GNNPRE_OK;
+}
+
+}  // namespace
+}  // namespace gnnpre
+
+using namespace gnnpre;
+
+extern "C" int64_t gnnpre_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int32_t steps) {
+    if (rows < 1 || cols < 1 || rows > kMaxSide || cols > kMaxSide || batch < 0 || batch > 16384 || steps < 1 || steps > kMaxSteps) return GNNPRE_ERR_INVALID_ARG;
+    if (batch == 0) return 0;
+    int64_t total = 0;
+    for (int32_t most = 1; most <= 3; ++most) total = std::max(total, ns_shape(batch, rows, cols, steps, most).total);
+    return total;
+}
+
+extern "C" int gnnpre_orthogonalize(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_stride, int64_t batch, int32_t dtype,
+                                    int32_t steps, const float* coeffs, float eps, float scale, void* out, int64_t ldo, int64_t o_stride,
+                                    void* workspace, int64_t workspace_bytes, int32_t* error_flag, void* stream) {
+    return ns_launch(G, rows, cols, ldg, g_stride, batch, dtype, steps, coeffs, eps, scale, out, ldo, o_stride, workspace, workspace_bytes,
+                     error_flag, stream);
+}
+
+// Failure-detection self-test: see include/gnnpre.h.
+extern "C" int gnnpre_orthogonalize_selftest_wait_timeout(const float* G, int64_t rows, int64_t cols, float* out, void* workspace,
+                                                          int64_t workspace_bytes, int32_t* error_flag, uint32_t polls, void* stream) {
+    if (!error_flag || polls == 0 || polls > 100000u) return GNNPRE_ERR_INVALID_ARG;
+    const float coeffs[3] = {1.5f, -0.5f, 0.f};
+    const NsSelfTest test{1, polls};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    GNNPRE_CUDA(cudaMemsetAsync(error_flag, 0, sizeof(int32_t), st));
+    GNNPRE_TRY(ns_launch(G, rows, cols, cols, 0, 1, GNNPRE_F32, 1, coeffs, 1e-7f, 1.f, out, cols, 0, workspace, workspace_bytes, error_flag, stream, &test));
+    GNNPRE_CUDA(cudaStreamSynchronize(st));
+    int32_t flag = 0;
+    GNNPRE_CUDA(cudaMemcpy(&flag, error_flag, sizeof(flag), cudaMemcpyDeviceToHost));
+    return flag ? GNNPRE_ERR_TIMEOUT : GNNPRE_OK;
+}

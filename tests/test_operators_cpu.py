@@ -63,3 +63,37 @@ def test_embedding_grad_workspace(lib):
     for n, dim, count in ((1, 1, 1), (1000, 64, 100), (169343, 128, 65553), ((1 << 31) - 1, 602, 2449029), (65536, 100, (1 << 31) - 1)):
         rows = (dim + 3) // 4 * 4
         assert 16 * count <= size(n, dim, count) <= 16 * count + rows * count + 8 * rows * 4 + count // 64 + (1 << 22) + (count // 4096 + 1) * 8192
+
+
+def coefficients(a=3.4445, b=-4.7750, c=2.0315):
+    import ctypes
+    return (ctypes.c_float * 3)(a, b, c)
+
+
+ORTH = dict(G=0x100000, rows=100, cols=60, ldg=60, g_stride=6000, batch=2, dtype=0, steps=5, coeffs=coefficients(), eps=1e-7, scale=1.0,
+            out=0x400000, ldo=60, o_stride=6000, workspace=0x4000000, workspace_bytes=1 << 30, error_flag=None, stream=None)
+
+
+@pytest.mark.parametrize("changes,status", [
+    (dict(G=None), INVALID_ARG), (dict(out=None), INVALID_ARG), (dict(workspace=None), INVALID_ARG), (dict(coeffs=None), INVALID_ARG),
+    (dict(rows=0), INVALID_ARG), (dict(cols=0), INVALID_ARG), (dict(rows=65537), INVALID_ARG), (dict(cols=65537, ldg=70000, ldo=70000), INVALID_ARG),
+    (dict(batch=-1), INVALID_ARG), (dict(batch=16385), INVALID_ARG), (dict(ldg=59), INVALID_ARG), (dict(ldo=59), INVALID_ARG),
+    (dict(g_stride=-1), INVALID_ARG), (dict(o_stride=5999), INVALID_ARG), (dict(dtype=3), INVALID_ARG), (dict(steps=0), INVALID_ARG),
+    (dict(steps=65), INVALID_ARG), (dict(eps=-1.0), INVALID_ARG), (dict(eps=float("nan")), INVALID_ARG), (dict(eps=float("inf")), INVALID_ARG),
+    (dict(coeffs=coefficients(a=float("nan"))), INVALID_ARG), (dict(coeffs=coefficients(b=float("inf"))), INVALID_ARG),
+    (dict(coeffs=coefficients(3.0, 3.0, 3.0)), INVALID_ARG), (dict(coeffs=coefficients(20.0, 0.0, 0.0)), INVALID_ARG),
+    (dict(workspace_bytes=1000), INVALID_ARG), (dict(workspace=0x4000080), ALIGN), (dict(G=0x100002), ALIGN), (dict(out=0x400001, dtype=1), ALIGN),
+    (dict(workspace=0x100000), INVALID_ARG), (dict(workspace=0x400000), INVALID_ARG), (dict(batch=0), 0)])
+def test_orthogonalize_refuses(lib, changes, status):
+    assert call(lib.gnnpre_orthogonalize, ORTH, **changes) == status
+
+
+def test_orthogonalize_workspace(lib):
+    size = lib.gnnpre_orthogonalize_workspace
+    assert size(0, 10, 10, 5) == 0
+    for args in ((-1, 10, 10, 5), (16385, 10, 10, 5), (1, 0, 10, 5), (1, 10, 0, 5), (1, 65537, 10, 5), (1, 10, 65537, 5), (1, 10, 10, 0), (1, 10, 10, 65)):
+        assert size(*args) == INVALID_ARG
+    assert size(3, 256, 602, 5) == size(3, 602, 256, 5)  # the smaller side counts, not which it is
+    for batch, rows, cols in ((1, 1, 1), (3, 256, 602), (1, 2048, 4096)):
+        r, n = (-(-x // 128) * 128 for x in sorted((rows, cols)))
+        assert 0 < size(batch, rows, cols, 5) <= batch * (4 * (3 * r * n + 5 * r * r) + 512) + 16384
