@@ -434,6 +434,46 @@ int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dtype, const v
                           int32_t table_dtype, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * Weight gradient of gnnpre_lc_first_layer on the mini-batch it was called with, summed over the hops:
+ *
+ *     dWt[h][f] = sum_k sum_i dZ_k[i][h] * hops[k][batch[i]][f]        (plus the old value with `accumulate`)
+ *     dZ_k[i][h] = dY_k[i][h] where Y_k[i][h] > 0 if bit k of relu_mask is set, dY_k[i][h] otherwise
+ *
+ *   hops, batch, relu_mask  as for gnnpre_lc_first_layer.  A batch index outside [0, n) is padding: it adds nothing, whatever dY
+ *                           holds there
+ *   dY          DEVICE fp32, the gradient of Y: element (k, i, h) at dY[k * dy_hop_stride + i * lddy + h]
+ *   Y           DEVICE fp32, what the forward call gave, laid out likewise; only hops of relu_mask are read (NULL if there are none)
+ *   dWt         DEVICE fp32 [hidden, feat_dim], leading dimension ldw: the gradient of Wt
+ *   workspace   DEVICE, 256-byte aligned, gnnpre_lc_first_layer_grad_workspace(num_hops, batch_size, feat_dim, hidden) bytes (which
+ *               returns a negative status for sizes that the call refuses).  In use until the call's work completes: one per
+ *               stream, and one per captured graph that may run beside others
+ *   error_flag  DEVICE int32 or NULL; set to 1 by the kernel if one of its bounded waits ran out (the results are then invalid).
+ *               The caller clears and reads it.
+ * hidden a multiple of 16, 16..256; 1 <= feat_dim <= 2^20; 0 <= batch_size < 2^31; strides not negative, ldh, ldw >= feat_dim, lddy,
+ * ldy >= hidden; dWt apart from what is read (else INVALID_ARG).  ldh a multiple of 4, hops 16-byte aligned, the other pointers
+ * aligned to their elements (else ALIGN).
+ * Arithmetic: operands enter with all 24 bits of fp32 (three bf16 numbers each, the six largest of the nine products), sums in fp32
+ * in a fixed order: results are bitwise reproducible on a device.  An operand that is not finite makes the sums it enters NaN.
+ * The work is enqueued on `stream` and the call returns without synchronising; nothing is allocated.
+ */
+int64_t gnnpre_lc_first_layer_grad_workspace(int32_t num_hops, int64_t batch_size, int64_t feat_dim, int64_t hidden);
+int gnnpre_lc_first_layer_grad(const float* const* hops, int32_t num_hops, int64_t n, int64_t feat_dim, int64_t ldh,
+                               const int32_t* batch, int64_t batch_size, const float* dY, int64_t lddy, int64_t dy_hop_stride,
+                               const float* Y, int64_t ldy, int64_t y_hop_stride, uint64_t relu_mask, int64_t hidden,
+                               int32_t accumulate, float* dWt, int64_t ldw, void* workspace, int64_t workspace_bytes,
+                               int32_t* error_flag, void* stream);
+
+/*
+ * Failure-detection self-test of gnnpre_lc_first_layer_grad's kernel, as gnnpre_lc_selftest_wait_timeout: the gradient over all n
+ * rows of one hop in which no finished chunk is announced, so that every bounded wait gives up after `polls` polls (1..100000).
+ * Synchronises; returns GNNPRE_ERR_TIMEOUT when the error word was raised (the expected outcome).  dWt receives nothing
+ * meaningful; workspace as for gnnpre_lc_first_layer_grad(1, n, feat_dim, hidden).
+ */
+int gnnpre_lc_grad_selftest_wait_timeout(const float* hop, int64_t n, int64_t feat_dim, int64_t ldh, const float* dY, int64_t lddy,
+                                         int64_t hidden, float* dWt, int64_t ldw, void* workspace, int64_t workspace_bytes,
+                                         int32_t* error_flag, uint32_t polls, void* stream);
+
+/*
  * An update orthogonalised by Newton-Schulz products (no counterpart in the paper: the step that turns the gradient of a weight
  * such as gnnpre_lc_first_layer's into an update whose singular values are all of one size).  For each of `batch` matrices
  *

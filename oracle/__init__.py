@@ -284,3 +284,21 @@ def orthogonalize(G, steps: int, coeffs, eps: float, scale: float) -> np.ndarray
         A = X @ np.swapaxes(X, -1, -2)
         X = a * X + b * (A @ X) + c * (A @ (A @ X))
     return scale * X
+
+
+def lc_first_layer_grad(hops, batch, dY, Y, relu_mask: int, want_abs: bool = False):
+    """sum_k dZ_k^T hops[k][batch] in fp64, dZ_k = dY_k where Y_k > 0 for the hops of relu_mask, dY_k for the others; a batch index
+    outside a hop matrix adds nothing (want_abs: also the sum of the terms' absolute values)."""
+    n = hops[0].shape[0]
+    batch = np.arange(n) if batch is None else np.asarray(batch, dtype=np.int64)
+    at = np.flatnonzero((batch >= 0) & (batch < n))
+    total = size = 0.0
+    for k, hop in enumerate(hops):
+        dz = np.asarray(dY[k], dtype=np.float64)[at]
+        if relu_mask >> k & 1:
+            dz = np.where(np.asarray(Y[k])[at] > 0, dz, 0.0)
+        x = np.asarray(hop, dtype=np.float64)[batch[at]]
+        total = total + dz.T @ x
+        if want_abs:
+            size = size + np.abs(dz).T @ np.abs(x)
+    return (total, size) if want_abs else total

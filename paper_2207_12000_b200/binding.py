@@ -103,6 +103,11 @@ def _load() -> ctypes.CDLL:
     lib.gnnpre_orthogonalize.argtypes = [p, i64, i64, i64, i64, i64, i32, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float,
                                          ctypes.c_float, p, i64, i64, p, i64, p, p]
     lib.gnnpre_orthogonalize_selftest_wait_timeout.argtypes = [p, i64, i64, p, p, i64, p, ctypes.c_uint32, p]
+    lib.gnnpre_lc_first_layer_grad_workspace.argtypes = [i32, i64, i64, i64]
+    lib.gnnpre_lc_first_layer_grad_workspace.restype = i64
+    lib.gnnpre_lc_first_layer_grad.argtypes = [ctypes.POINTER(ctypes.c_void_p), i32, i64, i64, i64, p, i64, p, i64, i64, p, i64, i64,
+                                               ctypes.c_uint64, i64, i32, p, i64, p, i64, p, p]
+    lib.gnnpre_lc_grad_selftest_wait_timeout.argtypes = [p, i64, i64, i64, p, i64, i64, p, i64, p, i64, p, ctypes.c_uint32, p]
     lib.gnnpre_normalize.argtypes = [p, p, i32, p]
     lib.gnnpre_solve_normalisation_blocks.argtypes = [i64] * 8 + [ctypes.POINTER(i64)]
     lib.gnnpre_selftest_wait_timeout.argtypes = [p, ctypes.c_uint32, p]
@@ -435,8 +440,7 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
     assert out.dtype in (d_out.dtype, torch.float32) and out.shape == (num_rows, D) and (out.stride(1) == 1 or D == 1)
     _on_current_device(d_out, ids, out)
     size = _lib.gnnpre_embedding_grad_workspace(num_rows, D, N)
-    room = _workspace(workspace, size, "gnnpre_embedding_grad",
-            "gnnpre_orthogonalize_workspace", "gnnpre_orthogonalize", "gnnpre_orthogonalize_selftest_wait_timeout", d_out.device)
+    room = _workspace(workspace, size, "gnnpre_embedding_grad", d_out.device)
     _on_current_device(room)
     _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), _rows(d_out), _DTYPES[d_out.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype], N,
                                       num_rows, D, scale, int(accumulate), out.data_ptr(), _rows(out), _DTYPES[out.dtype],
@@ -444,6 +448,89 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
     if workspace is None and stream is not None:
         room.record_stream(stream)  # allocated on the current stream, used on another
     return out
+
+
+def gnnpre_lc_first_layer_grad_workspace(num_hops: int, batch_size: int, feat_dim: int, hidden: int) -> int:
+    """Bytes of workspace that gnnpre_lc_first_layer_grad needs."""
+    size = _lib.gnnpre_lc_first_layer_grad_workspace(num_hops, batch_size, feat_dim, hidden)
+    if size < 0:
+        raise GnnpreError(size, "gnnpre_lc_first_layer_grad_workspace")
+    return size
+
+
+def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor | None = None, relu_mask: int = 0,
+                               out: torch.Tensor | None = None, accumulate: bool = False, concat: bool = False,
+                               workspace: torch.Tensor | None = None, check: bool = True, stream=None) -> torch.Tensor:
+    """Gradient of gnnpre_lc_first_layer in its weight, [H, F]: sum over the hops of dZ_k.T @ hops[k][batch], dZ_k = dY_k where Y_k > 0
+    for the hops of relu_mask, dY_k for the others.
+
+    hops, batch as in the forward call; dY and Y (its result; needed with relu_mask) are [K, B, H], or [B, K*H] with concat=True.  With
+    accumulate=True the gradient is added to out.  workspace: uint8 tensor of gnnpre_lc_first_layer_grad_workspace bytes, for callers
+    that keep one.  With check=True the call synchronises and raises if a device-side wait ran out."""
+    K = len(hops)
+    shape, hs = hops[0].shape, hops[0].stride()
+    n, F = shape
+    assert hs[1] == 1 or F == 1
+    for h in hops:
+        assert h.dtype is torch.float32 and h.shape == shape and h.stride() == hs
+    if batch is None:
+        N, bptr = n, None
+    else:
+        if batch.dtype is torch.int64:
+            batch = batch.to(torch.int32)
+        assert batch.dtype is torch.int32 and batch.dim() == 1 and batch.is_contiguous()
+        N, bptr = batch.shape[0], batch.data_ptr()
+        _on_current_device(batch)
+    H = dY.shape[-1] // K if concat else dY.shape[-1]
+
+    def layout(t):  # (leading dimension, distance between the hops)
+        assert t.dtype is torch.float32 and t.shape == ((N, K * H) if concat else (K, N, H)) and t.stride(-1) == 1
+        if concat:
+            return _rows(t), H
+        return max(t.stride(1), H) if N <= 1 else t.stride(1), max(t.stride(0), 0)
+
+    lddy, dy_hop = layout(dY)
+    assert Y is not None or not relu_mask
+    ldy, y_hop = layout(Y) if Y is not None else (0, 0)
+    assert out is not None or not accumulate
+    if out is None:
+        out = torch.empty((H, F), dtype=torch.float32, device=dY.device)
+    assert out.dtype is torch.float32 and out.shape == (H, F) and (out.stride(1) == 1 or F == 1)
+    _on_current_device(dY, out, *hops)
+    if Y is not None:
+        _on_current_device(Y)
+    size = _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H)
+    room = _workspace(workspace, size, "gnnpre_lc_first_layer_grad", dY.device)
+    _on_current_device(room)
+    flag = torch.zeros(1, dtype=torch.int32, device=dY.device) if check else None
+    if check and stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())  # the flag is cleared on the current one
+    _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, hs[0], bptr, N, dY.data_ptr(), lddy, dy_hop,
+                                           Y.data_ptr() if Y is not None else None, ldy, y_hop, relu_mask, H, int(accumulate), out.data_ptr(),
+                                           _rows(out), room.data_ptr(), room.numel(), flag.data_ptr() if check else None, _stream_ptr(stream)),
+           "gnnpre_lc_first_layer_grad")
+    if workspace is None and stream is not None:
+        room.record_stream(stream)
+    if check:
+        if stream is not None:
+            stream.synchronize()
+        if int(flag.item()) != 0:
+            raise GnnpreError(-8, "gnnpre_lc_first_layer_grad")
+    return out
+
+
+def gnnpre_lc_grad_selftest_wait_timeout(hop: torch.Tensor, dY: torch.Tensor, polls: int = 200, stream=None) -> int:
+    """Status of a weight gradient whose waits are made to run out (expected: -8, GNNPRE_ERR_TIMEOUT)."""
+    n, F = hop.shape
+    H = dY.shape[1]
+    assert dY.shape[0] == n
+    out = torch.empty((H, F), dtype=torch.float32, device=hop.device)
+    room = torch.empty(gnnpre_lc_first_layer_grad_workspace(1, n, F, H), dtype=torch.uint8, device=hop.device)
+    flag = torch.zeros(1, dtype=torch.int32, device=hop.device)
+    _on_current_device(hop, dY)
+    return int(_lib.gnnpre_lc_grad_selftest_wait_timeout(hop.data_ptr(), n, F, hop.stride(0), dY.data_ptr(), dY.stride(0), H,
+                                                         out.data_ptr(), F, room.data_ptr(), room.numel(), flag.data_ptr(), polls,
+                                                         _stream_ptr(stream)))
 
 
 def gnnpre_orthogonalize_workspace(batch: int, rows: int, cols: int, steps: int) -> int:
@@ -594,6 +681,8 @@ def exported_symbols():
     return ["gnnpre_degrees", "gnnpre_build_plan", "gnnpre_plan_info", "gnnpre_plan_block", "gnnpre_plan_scales",
             "gnnpre_plan_support", "gnnpre_plan_hop_order", "gnnpre_propagate", "gnnpre_propagate_weighted", "gnnpre_hop_static", "gnnpre_lc_first_layer", "gnnpre_lc_selftest_wait_timeout", "gnnpre_normalize",
             "gnnpre_embedding_lookup", "gnnpre_embedding_grad_workspace", "gnnpre_embedding_grad",
+            "gnnpre_lc_first_layer_grad_workspace", "gnnpre_lc_first_layer_grad", "gnnpre_lc_grad_selftest_wait_timeout",
+            "gnnpre_orthogonalize_workspace", "gnnpre_orthogonalize", "gnnpre_orthogonalize_selftest_wait_timeout",
             "gnnpre_solve_normalisation_blocks", "gnnpre_selftest_wait_timeout", "gnnpre_selftest_wait_timeout_async",
             "gnnpre_plan_status", "gnnpre_inject_alloc_failure", "gnnpre_gather_ceiling", "gnnpre_describe_panels", "gnnpre_plan_destroy", "gnnpre_release_cached_memory", "gnnpre_solve_budget",
             "gnnpre_status_string", "gnnpre_last_cuda_error"]

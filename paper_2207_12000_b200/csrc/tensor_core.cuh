@@ -70,10 +70,17 @@ __device__ __forceinline__ uint64_t tc_desc_k(uint32_t addr) {
            ((uint64_t)2 << 61);
 }
 
-// fp32 accumulator; both operands fp16 (or bf16), K-major unless told; M rows, N columns.
-__device__ __forceinline__ uint32_t tc_instr(int m, int n, bool bf16, bool mn_major = false) {
-    const uint32_t type = bf16 ? 1u : 0u, major = mn_major ? 1u : 0u;
-    return (1u << 4) | (type << 7) | (type << 10) | (major << 15) | (major << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+// Operand B as it lies in a row-major [K, N] matrix (MN-major): blocks of 64 neighbouring columns, `block_bytes` apart, whose rows
+// (one per element of K) are 128 bytes in the 128-byte swizzle; a step of 16 along K adds 2048 bytes.
+__device__ __forceinline__ uint64_t tc_desc_mn(uint32_t addr, uint32_t block_bytes) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(block_bytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+           ((uint64_t)2 << 61);
+}
+
+// fp32 accumulator; both operands fp16 (or bf16), A K-major, B K-major unless told; M rows, N columns.
+__device__ __forceinline__ uint32_t tc_instr(int m, int n, bool bf16, bool b_mn_major = false) {
+    const uint32_t type = bf16 ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
 // Called by a whole warp, issued by one elected lane (always the same).
@@ -84,6 +91,17 @@ __device__ __forceinline__ void tc_mma(uint32_t tmem_d, uint64_t a, uint64_t b, 
         "setp.ne.b32 p, %4, 0;\n\t"
         "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
         "l"(a), "l"(b), "r"(instr), "r"(accumulate)
+        : "memory");
+}
+
+// The same with A in tensor memory: row = lane, two elements of K per 32-bit column.
+__device__ __forceinline__ void tc_mma_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t b, uint32_t instr, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+        "r"(tmem_a), "l"(b), "r"(instr), "r"(accumulate)
         : "memory");
 }
 
@@ -115,6 +133,16 @@ __device__ __forceinline__ void tc_load32(uint32_t taddr, uint32_t (&v)[32]) {
         : "memory");
 }
 
+// 16 neighbouring columns of this thread's lane; complete after tc_store_wait.
+__device__ __forceinline__ void tc_store16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(v[0]),
+        "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tc_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }

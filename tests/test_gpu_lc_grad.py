@@ -1,0 +1,216 @@
+"""gnnpre_lc_first_layer_grad against the oracle.
+
+Integers whose sums fp32 holds are compared bit for bit: gather, mask, operand layouts and the shares of the batch.  On normal inputs
+the error is bounded by the terms' absolute values: a term's operands enter whole, the dropped products are below 2^-23 of it;
+inside the tensor core a term meets at most 32 sums that are cut at 2^-23 of their size; the sums of 64 rows are then added,
+rounded to nearest (2^-24), at most once per 64 rows and hop within a share and at most 192 times between shares.
+"""
+import numpy as np
+import pytest
+import torch
+
+import gnnpre_inputs as gi
+import oracle as orc
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2207_12000_b200 import binding
+    return binding
+
+
+def padded(M, pad, rows_too=0, fill=float("nan")):
+    """Device copy of a host array, its rows inside longer ones full of `fill`."""
+    M = torch.as_tensor(np.ascontiguousarray(M))
+    *lead, r, c = M.shape
+    buf = torch.full((*lead, r + rows_too, c + pad), fill, dtype=torch.float32, device="cuda")
+    view = buf[..., :r, :c]
+    view.copy_(M)
+    return view
+
+
+def aligned(M):
+    """The same with rows that start on 16-byte boundaries (hop matrices)."""
+    return padded(M, 4 + -M.shape[1] % 4)
+
+
+SHAPES = [
+    # n, F, H, batch size (None = every row), hops
+    (1000, 32, 16, 128, 1), (64, 16, 128, 32, 1), (40, 5, 32, 1, 2), (5000, 100, 256, 4096, 3), (3000, 128, 256, 1000, 2),
+    (777, 13, 48, 300, 2), (2000, 602, 64, 517, 1), (517, 40, 80, None, 2), (900, 300, 192, 333, 1), (400, 129, 144, 31, 9),
+    (60000, 100, 256, 50001, 3), (30, 1, 16, 33, 1), (2000, 2500, 256, 70, 1), (300, 20, 240, 20000, 1)]
+
+
+def case(n, F, H, bs, K, seed, integers):
+    rng = np.random.default_rng(seed)
+    draw = (lambda *s: rng.integers(-3, 4, size=s).astype(np.float32)) if integers else (lambda *s: rng.standard_normal(s, dtype=np.float32))
+    rows = n if bs is None else bs
+    hops = [draw(n, F) for _ in range(K)]
+    dY, Y = draw(K, rows, H), draw(K, rows, H)
+    if bs is None:
+        return hops, None, dY, Y
+    batch = rng.integers(0, n, size=bs)
+    if bs > 20:  # padding, on both sides of the matrix, with what must not be looked at
+        batch[rng.random(bs) < 0.05] = -1
+        batch[rng.random(bs) < 0.05] = n
+        batch[5], batch[6] = np.iinfo(np.int32).max, np.iinfo(np.int32).min
+        dY[:, (batch < 0) | (batch >= n)] = np.nan
+    return hops, batch, dY, Y
+
+
+@pytest.mark.parametrize("n,F,H,bs,K", SHAPES)
+def test_exact_on_integers(B, n, F, H, bs, K):
+    hops, batch, dY, Y = case(n, F, H, bs, K, n + F, True)
+    mask = 0b1010110110
+    d_hops = [aligned(h) for h in hops]
+    d_batch = None if batch is None else torch.from_numpy(batch.astype(np.int32)).cuda()
+    want = orc.lc_first_layer_grad(hops, batch, dY, Y, mask)
+    # what lies where the mask leaves nothing is not looked at either
+    dY_masked = dY.copy()
+    for k in range(K):
+        if mask >> k & 1:
+            dY_masked[k][Y[k] <= 0] = np.inf
+    got = B.gnnpre_lc_first_layer_grad(d_hops, d_batch, padded(dY_masked, 3, 1), Y=padded(Y, 1, 2), relu_mask=mask)
+    assert got.shape == (H, F) and np.array_equal(got.cpu().double().numpy(), want)
+    # hops side by side, a strided result, added to what is there
+    side = np.concatenate(list(dY_masked), axis=1), np.concatenate(list(Y), axis=1)
+    old = np.random.default_rng(1).integers(-5, 6, size=(H, F)).astype(np.float32)
+    out = padded(old, 3)
+    B.gnnpre_lc_first_layer_grad(d_hops, d_batch, padded(side[0], 2), Y=padded(side[1], 2), relu_mask=mask, concat=True, out=out, accumulate=True)
+    assert np.array_equal(out.cpu().double().numpy(), want + old)
+    assert torch.isnan(out._base[:, F:]).all()
+
+
+@pytest.mark.parametrize("n,F,H,bs,K", SHAPES)
+def test_normal_inputs_within_the_bound(B, n, F, H, bs, K):
+    hops, batch, dY, Y = case(n, F, H, bs, K, n + H, False)
+    dY *= np.float32(1e-20)  # any scale fits
+    mask = 0b11110
+    got = B.gnnpre_lc_first_layer_grad([aligned(h) for h in hops], None if batch is None else torch.from_numpy(batch).cuda(),
+                                       torch.from_numpy(dY).cuda(), Y=torch.from_numpy(Y).cuda(), relu_mask=mask)
+    want, size = orc.lc_first_layer_grad(hops, batch, dY, Y, mask, want_abs=True)
+    rows = n if bs is None else bs
+    bound = (33 * 2.0 ** -23 + (K * (rows / 64 + 1) + 192) * 2.0 ** -24) * size
+    err = np.abs(got.cpu().double().numpy() - want)
+    assert (err <= bound).all(), float((err / np.maximum(bound, 1e-300)).max())
+    # and far below what one product of bf16 or tf32 numbers would give: 2^-18 of the result's size
+    assert np.linalg.norm(err) <= 2.0 ** -18 * np.linalg.norm(want)
+
+
+def test_is_the_forward_calls_gradient(B):
+    """The layer is linear in its weight where the signs of Y do not change: <dY, Y(W + D) - Y(W)> = <dW, D>.  Integers: exact."""
+    rng = np.random.default_rng(5)
+    hops = [aligned(rng.integers(0, 4, size=(700, 36)).astype(np.float32)) for _ in range(2)]
+    W, D = (torch.from_numpy(rng.integers(lo, 5, size=(48, 36)).astype(np.float32)).cuda() for lo in (0, 0))
+    W[::3] *= -1  # outputs that are never positive, before and after
+    D[::3] *= -1
+    batch = torch.from_numpy(rng.integers(0, 700, size=501).astype(np.int32)).cuda()
+    mask = 0b10
+    Y, Y2 = (B.gnnpre_lc_first_layer(hops, batch, w, relu_mask=mask) for w in (W, W + D))
+    dY = torch.from_numpy(rng.integers(-3, 4, size=(2, 501, 48)).astype(np.float32)).cuda()
+    same = (Y > 0) == (Y2 > 0)
+    dY[~same] = 0  # (rows of zeros that D brings above zero)
+    dW = B.gnnpre_lc_first_layer_grad(hops, batch, dY, Y=Y, relu_mask=mask)
+    assert float(((Y2 - Y).double() * dY.double()).sum()) == float((dW.double() * D.double()).sum())
+
+
+def test_empty_batch_and_no_relu(B):
+    hop = aligned(np.ones((10, 7), dtype=np.float32))
+    none = torch.empty((1, 0, 16), device="cuda")
+    batch = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert (B.gnnpre_lc_first_layer_grad([hop], batch, none) == 0).all()
+    kept = torch.full((16, 7), 2.0, device="cuda")
+    assert (B.gnnpre_lc_first_layer_grad([hop], batch, none, out=kept, accumulate=True) == 2).all()
+    dY = torch.ones((1, 10, 16), device="cuda")
+    assert (B.gnnpre_lc_first_layer_grad([hop], None, dY) == 10).all()
+    batch = torch.full((10,), -1, dtype=torch.int32, device="cuda")
+    assert (B.gnnpre_lc_first_layer_grad([hop], batch, dY) == 0).all()
+
+
+def test_not_finite_operands_reach_their_sums(B):
+    hop = aligned(np.ones((40, 20), dtype=np.float32))
+    dY = torch.ones((1, 40, 16), device="cuda")
+    dY[0, 7, 3] = float("nan")
+    hop[9, 4] = float("inf")
+    got = B.gnnpre_lc_first_layer_grad([hop], None, dY)
+    bad = torch.zeros((16, 20), dtype=torch.bool, device="cuda")
+    bad[3], bad[:, 4] = True, True
+    assert not torch.isfinite(got[bad]).any() and (got[~bad] == 40).all()
+
+
+def test_reproducible_in_a_graph_and_on_a_stream(B):
+    hops, batch, dY, Y = case(3000, 77, 96, 5000, 2, 3, False)
+    args = [aligned(h) for h in hops], torch.from_numpy(batch.astype(np.int32)).cuda(), torch.from_numpy(dY).cuda()
+    y = torch.from_numpy(Y).cuda()
+    first = B.gnnpre_lc_first_layer_grad(*args, Y=y, relu_mask=2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert torch.equal(B.gnnpre_lc_first_layer_grad(*args, Y=y, relu_mask=2, stream=side), first)
+    out = torch.empty_like(first)
+    room = torch.empty(B.gnnpre_lc_first_layer_grad_workspace(2, 5000, 77, 96), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.gnnpre_lc_first_layer_grad(*args, Y=y, relu_mask=2, out=out, workspace=room, check=False)
+    for _ in range(2):
+        out.fill_(7.0), room.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
+
+
+def test_waits_that_run_out_are_reported_and_leave_the_device_usable(B):
+    hop, dY = aligned(np.ones((1000, 150), dtype=np.float32)), torch.ones((1000, 144), device="cuda")
+    assert B.gnnpre_lc_grad_selftest_wait_timeout(hop, dY, polls=50) == -8
+    assert (B.gnnpre_lc_first_layer_grad([hop], None, dY[None]) == 1000).all()
+
+
+def test_a_training_step_of_the_first_stage(B):
+    """Categories to features, hops, first stage, its gradients and an orthogonalised update, each against the oracle on what the
+    step before it gave."""
+    rng = np.random.default_rng(3)
+    g = gi.rmat(3000, 9000, 4, directed_candidates=False)
+    kinds, F, H, K = 200, 44, 64, 2
+    table = torch.from_numpy(rng.standard_normal((kinds, F), dtype=np.float32)).cuda()
+    ids_np = rng.integers(-1, kinds, size=g.n)
+    ids = torch.from_numpy(ids_np).cuda()
+    X0 = B.gnnpre_embedding_lookup(table, ids, scale=0.5)
+    plan = B.gnnpre_build_plan(g.rowptr.cuda(), g.colidx.cuda(), B.GNNPRE_OP_GCN_SYM, F)
+    hops, _ = B.gnnpre_propagate(plan, X0, K)
+    batch_np = rng.permutation(g.n)[:700]
+    batch = torch.from_numpy(batch_np.astype(np.int32)).cuda()
+    Wt = torch.from_numpy((rng.standard_normal((H, F)) / np.sqrt(F)).astype(np.float32)).cuda()
+    Y = B.gnnpre_lc_first_layer(hops, batch, Wt, relu_mask=0b10, precision=B.GNNPRE_LC_TF32X3)
+    dY = torch.from_numpy(rng.standard_normal((K, 700, H), dtype=np.float32) / 700).cuda()
+    dW = B.gnnpre_lc_first_layer_grad(hops, batch, dY, Y=Y, relu_mask=0b10)
+    wide = lambda t: t.cpu().numpy()  # noqa: E731
+    want, size = orc.lc_first_layer_grad([wide(h) for h in hops], batch_np, wide(dY), wide(Y), 0b10, want_abs=True)
+    assert (np.abs(wide(dW).astype(np.float64) - want) <= (33 * 2.0 ** -23 + (K * 12 + 192) * 2.0 ** -24) * size).all()
+    update = B.gnnpre_orthogonalize(dW, scale=0.2)
+    ortho = orc.orthogonalize(wide(dW), 5, tuple(float(np.float32(c)) for c in (3.4445, -4.7750, 2.0315)), 1e-7, float(np.float32(0.2)))
+    assert np.linalg.norm(wide(update) - ortho) <= 2.0 ** -12 * np.linalg.norm(ortho)
+    Wt -= update
+    # back to the table: dX_k = dZ_k W_1 (the first stage itself, with the weight's other side), through the hops (the GCN filter is
+    # symmetric), to the categories
+    dZ = torch.where((Y > 0) | (torch.arange(K, device="cuda") == 0)[:, None, None], dY, 0.0)
+    every = [torch.zeros((g.n, H), device="cuda").index_copy_(0, batch.long(), dZ[k]) for k in range(K)]
+    back = B.gnnpre_lc_first_layer(every, None, (Wt + update).t().contiguous()[:32], precision=B.GNNPRE_LC_TF32X3)
+    d1, _ = B.gnnpre_propagate(B.gnnpre_build_plan(g.rowptr.cuda(), g.colidx.cuda(), B.GNNPRE_OP_GCN_SYM, 32), back[0].contiguous(), 1)
+    d2, _ = B.gnnpre_propagate(B.gnnpre_build_plan(g.rowptr.cuda(), g.colidx.cuda(), B.GNNPRE_OP_GCN_SYM, 32), back[1].contiguous(), 2)
+    dX0 = d1[0] + d2[1]
+    d_table = B.gnnpre_embedding_grad(dX0, ids, kinds, scale=0.5)
+    want, size, terms = orc.embedding_grad(wide(dX0), ids_np, kinds, 0.5, want_abs=True)
+    assert (np.abs(wide(d_table).astype(np.float64) - want) <= (terms[:, None] + 3) * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want)).all()
+    # the step descends: <d_table, D> is the change of <dY, Y> along D in the columns that were carried back, to rounding
+    D = torch.zeros_like(table)
+    D[:, :32] = d_table
+    D *= 1e-2 / D.norm()
+    W_old = Wt + update
+    lin = lambda t: sum((torch.where((Y[k] > 0) | (k == 0), (h[batch.long()].double() @ W_old.double().t()), 0.0) * dY[k].double()).sum()  # noqa: E731
+                        for k, h in enumerate(B.gnnpre_propagate(plan, B.gnnpre_embedding_lookup(t, ids, scale=0.5), K)[0]))
+    slope = float(lin(table + D) - lin(table - D)) / 2
+    assert abs(slope - float((d_table.double() * D[:, :32].double()).sum())) <= 1e-4 * abs(slope)
+    plan.close()

@@ -97,3 +97,39 @@ def test_orthogonalize_workspace(lib):
     for batch, rows, cols in ((1, 1, 1), (3, 256, 602), (1, 2048, 4096)):
         r, n = (-(-x // 128) * 128 for x in sorted((rows, cols)))
         assert 0 < size(batch, rows, cols, 5) <= batch * (4 * (3 * r * n + 5 * r * r) + 512) + 16384
+
+
+def pointers(*p):
+    import ctypes
+    return (ctypes.c_void_p * len(p))(*p)
+
+
+LC_GRAD = dict(hops=pointers(0x100000, 0x200000), num_hops=2, n=1000, feat_dim=60, ldh=64, batch=0x900000, batch_size=100, dY=0x910000, lddy=32,
+               dy_hop_stride=3200, Y=0x920000, ldy=32, y_hop_stride=3200, relu_mask=2, hidden=32, accumulate=0, dWt=0x930000, ldw=60,
+               workspace=0x4000000, workspace_bytes=1 << 30, error_flag=None, stream=None)
+
+
+@pytest.mark.parametrize("changes,status", [
+    (dict(hops=None), INVALID_ARG), (dict(hops=pointers(0x100000, None)), INVALID_ARG), (dict(hops=pointers(0x100000, 0x200008)), ALIGN),
+    (dict(num_hops=0), INVALID_ARG), (dict(num_hops=65), INVALID_ARG), (dict(n=0), INVALID_ARG), (dict(n=1 << 31), INVALID_ARG),
+    (dict(feat_dim=0), INVALID_ARG), (dict(feat_dim=(1 << 20) + 4, ldh=1 << 21, ldw=1 << 21), INVALID_ARG), (dict(ldh=56), INVALID_ARG),
+    (dict(ldh=62), ALIGN), (dict(ldw=59), INVALID_ARG), (dict(lddy=31), INVALID_ARG), (dict(ldy=31), INVALID_ARG), (dict(dy_hop_stride=-4), INVALID_ARG),
+    (dict(y_hop_stride=-4), INVALID_ARG), (dict(batch_size=-1), INVALID_ARG), (dict(batch_size=1 << 31), INVALID_ARG),
+    (dict(batch=None, batch_size=1001), INVALID_ARG), (dict(dY=None), INVALID_ARG), (dict(Y=None), INVALID_ARG), (dict(dWt=None), INVALID_ARG),
+    (dict(workspace=None), INVALID_ARG), (dict(workspace_bytes=100), INVALID_ARG), (dict(workspace=0x4000040), ALIGN), (dict(hidden=8), INVALID_ARG),
+    (dict(hidden=24), INVALID_ARG), (dict(hidden=272, lddy=272, ldy=272), INVALID_ARG), (dict(dY=0x910002), ALIGN), (dict(Y=0x920001), ALIGN),
+    (dict(dWt=0x930002), ALIGN), (dict(batch=0x900002), ALIGN), (dict(dWt=0x910000), INVALID_ARG), (dict(dWt=0x920000), INVALID_ARG),
+    (dict(dWt=0x900000), INVALID_ARG), (dict(dWt=0x200000), INVALID_ARG), (dict(dWt=0x4000000), INVALID_ARG)])
+def test_lc_grad_refuses(lib, changes, status):
+    assert call(lib.gnnpre_lc_first_layer_grad, LC_GRAD, **changes) == status
+
+
+def test_lc_grad_workspace(lib):
+    size = lib.gnnpre_lc_first_layer_grad_workspace
+    assert size(3, 0, 100, 256) == 0
+    for args in ((0, 1, 1, 16), (65, 1, 1, 16), (1, -1, 1, 16), (1, 1 << 31, 1, 16), (1, 1, 0, 16), (1, 1, (1 << 20) + 1, 16), (1, 1, 1, 0),
+                 (1, 1, 1, 20), (1, 1, 1, 272)):
+        assert size(*args) == INVALID_ARG
+    for K, rows, F, H in ((1, 1, 1, 16), (3, 4096, 128, 256), (2, 20011, 602, 192), (3, 2449029, 100, 256)):
+        tiles = -(-H // 128) * -(-F // 128)
+        assert 0 < size(K, rows, F, H) <= 4 * max(1, 192 // tiles) * H * (F + 16 * -(-F // 128))
