@@ -8,13 +8,17 @@
 //
 //   warps 0-7    add up.  They read finished accumulators out of tensor memory and add them, rounded to nearest, to sums in
 //                registers (the tensor core cuts what an addition drops, so long sums in one accumulator come out too small).
-//   warps 8-11   operand A = dZ^T: a lane has one column h and reads it in the 32 rows of a chunk, masks, splits, and stores it to
+//   warps 8-15   operand A = dZ^T: a lane has one column h and reads it in the 16 rows of a chunk, masks, splits, and stores it to
 //                tensor memory, where a lane is a row of A.
-//   warps 12-15  operand B = the gathered rows of X: split and laid down in shared memory as they lie, rows along K.
-//   warps 16-19  copy chunks of dY, Y and the gathered rows into shared memory, asynchronously and as many chunks ahead as there is
-//                room for: no register holds what is in flight, and zeros fill what does not exist.  (Read by the splitting warps
-//                themselves, 32 rows at a time: 9.2 us a chunk, 28.6 ms for 2.4 M rows x 3 hops, F = 100, hidden 256.)
-//   warp 20      issues the products.
+//   warps 16-23  operand B = the gathered rows of X: split and laid down in shared memory as they lie, rows along K.
+//                Splitting a chunk is a chain of waits, reads, splits and stores, so either kind has two groups of four warps that
+//                take the chunks in turn.
+//   warps 24-26  have the copy engine bring chunks into shared memory, as many ahead as there is room for: 24 and 25, in turn, gathered
+//                rows of X (four per instruction), 26 tiles of dY and Y.  One warp issues a chunk's copies in some 1,200 cycles, of
+//                which the copies' own instructions are the least; read by the splitting warps themselves the rows took 9.2 us a
+//                chunk of 32, 16-byte copies by four warps (cp.async) 1.7 us.  Rows of dY or Y that do not start on 16-byte
+//                boundaries take 4-byte copies by warps 24 and 25.
+//   warp 27      issues the products.
 //
 // Numbers.  An fp32 operand is the sum of three bf16 numbers, cut one after the other from its 24 bits, so nothing is lost and any
 // scale fits; of the nine products the six largest are taken, which drops less than 2^-23 of |dZ||X| per term.  (Two fp16 numbers
@@ -33,25 +37,31 @@ namespace gnnpre {
 namespace {
 
 constexpr int kGradTile = 128;        // rows (h) of a tile, columns (f) at most
-constexpr int kGradChunk = 32;        // batch rows per stage
-constexpr int kGradRaw = 3;           // chunks being copied or split
-constexpr int kGradStages = 3;        // chunks split
-constexpr int kGradSlice = 2;         // chunks whose products share an accumulator
-constexpr int kGradSumWarps = 8, kGradBWarp = 12, kGradCopyWarp = 16, kGradMmaWarp = 20, kGradWarps = 24;
+constexpr int kGradChunk = 16;        // batch rows per stage
+constexpr int kGradMaxHops = 8;       // hops per launch
+constexpr int kGradRaw = 6;           // chunks being copied or split
+constexpr int kGradStages = 6;        // chunks split
+constexpr int kGradSlice = 4;         // chunks whose products share an accumulator
+constexpr int kGradSumWarps = 8, kGradBWarp = 16, kGradCopyWarp = 24, kGradTileWarp = 26, kGradMmaWarp = 27, kGradWarps = 28;
 constexpr int kGradThreads = 32 * kGradWarps;            // (whole warpgroups, for the registers they hand on)
-constexpr uint32_t kGradMatrix = kGradChunk * kGradTile * 4;  // a chunk of dY, Y or X as copied: 32 rows of 512 bytes
+constexpr uint32_t kGradAllRows = (1u << kGradChunk) - 1;
+constexpr uint32_t kGradMatrix = kGradChunk * kGradTile * 4;  // a chunk of dY, Y or X as copied: rows of 512 bytes
 constexpr uint32_t kGradRawStage = 3 * kGradMatrix;
-constexpr uint32_t kGradPart = 2 * kGradChunk * 128;     // one part of B's chunk: two blocks of 64 columns, 32 rows of 128 bytes
+constexpr uint32_t kGradPart = 2 * kGradChunk * 128;     // one part of B's chunk: two blocks of 64 columns, rows of 128 bytes
 constexpr uint32_t kGradStage = 3 * kGradPart;
-constexpr uint32_t kGradTmem = 512, kGradTmemA = 256, kGradTmemStage = 48;
+constexpr uint32_t kGradTmem = 512, kGradTmemA = 256, kGradTmemStage = 24;
 constexpr int kGradSmem = kGradStages * (int)kGradStage + kGradRaw * (int)kGradRawStage + 1024;
-// Registers per thread: 768 threads start with 80, 61,440 in all; 2 x 128 x 104 + 128 x (96 + 80 + 56 + 24) = 59,392.
-constexpr int kRegsSum = 104, kRegsA = 96, kRegsCopy = 56, kRegsMma = 24;
+// Registers per thread: 896 threads start with 72, 64,512 in all = 256 x (104 + 72 + 48) + 128 x 56.
+constexpr int kRegsSum = 104, kRegsB = 48, kRegsRest = 56;
+
+struct GradMaps {
+    CUtensorMap x[kGradMaxHops];  // [n, F] hop matrices, box [1, 128]
+    CUtensorMap dy, y;            // [hops, batch_size, hidden], box [1, 16, 128]
+};
 
 struct GradArgs {
-    const float* hop[GNNPRE_MAX_HOPS];
-    int64_t ldh, n;
-    int32_t feat_dim, hidden, num_hops;
+    int64_t n;
+    int32_t feat_dim, hidden;
     const int32_t* batch;
     int64_t batch_size;
     const float* dy;
@@ -62,7 +72,8 @@ struct GradArgs {
     int32_t tiles_f, width;     // tiles of `width` features (a multiple of 16)
     int32_t tiles;              // of dWt
     int32_t splits;
-    int64_t chunks_per_hop, chunks;
+    int32_t chunks_per_hop;
+    int64_t chunks;
     float* parts;               // [splits][hidden][part_ld]
     int64_t part_ld;
     int32_t* error;
@@ -95,12 +106,26 @@ __device__ __forceinline__ void fewer_registers() {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
-// BYTES bytes global -> shared without passing through registers, or as many zeros.
-template <int BYTES>
+// Four bytes global -> shared without passing through registers, or as many zeros.
 __device__ __forceinline__ void grad_copy(uint32_t dst, const float* src, bool live) {
-    const int size = live ? BYTES : 0;
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+    const int size = live ? 4 : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
+
+// Four rows of X, and a chunk of dY or Y; what lies outside the matrices comes as zeros.
+__device__ __forceinline__ void grad_gather4(uint32_t dst, const CUtensorMap* map, int x0, int r0, int r1, int r2, int r3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x0), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+        : "memory");
+}
+__device__ __forceinline__ void grad_tile(uint32_t dst, const CUtensorMap* map, int x0, int y0, int z0, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x0), "r"(y0), "r"(z0)
+        : "memory");
 }
 
 __device__ __forceinline__ float4 grad_read4(uint32_t at) {
@@ -114,11 +139,12 @@ __device__ __forceinline__ float grad_read(uint32_t at) {
     return v;
 }
 
-__global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_constant__ GradArgs a) {
+__global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_constant__ GradMaps maps, const __grid_constant__ GradArgs a) {
     extern __shared__ unsigned char grad_smem[];
     __shared__ __align__(8) unsigned long long bars[2 * kGradStages + 2 * kGradRaw + 5];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
+    __shared__ uint32_t rows_of[kGradRaw];  // of a chunk as copied: the rows that exist
     volatile int* abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (tc_smem(grad_smem) + 1023u) & ~1023u;
@@ -138,7 +164,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
             tc_bar_init(empty(s), 1);
         }
         for (int s = 0; s < kGradRaw; ++s) {
-            tc_bar_init(raw_full(s), 128);               // every copying thread, once its copies have landed
+            tc_bar_init(raw_full(s), a.wide ? 2 : 1 + 32);  // X and the tiles, or X and every thread that copies
             tc_bar_init(raw_empty(s), 8);
         }
         for (int b = 0; b < 2; ++b) {
@@ -160,7 +186,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
     const int h0 = tile / a.tiles_f * kGradTile, f0 = tile % a.tiles_f * a.width;
     const int64_t first = a.chunks * split / a.splits, last = a.chunks * (split + 1) / a.splits;
     const int count = (int)(last - first), slices = (count + kGradSlice - 1) / kGradSlice;
-    auto hop_of = [&](int64_t chunk) { return (int)(chunk / a.chunks_per_hop); };
+    // the share's first chunk; the others follow one by one
+    int hop = (int)(first / a.chunks_per_hop);
+    int in_hop = (int)(first - (int64_t)hop * a.chunks_per_hop);
+    auto advance = [&](int& k, int& c) {
+        if (++c == a.chunks_per_hop) {
+            c = 0;
+            ++k;
+        }
+    };
 
     if (warp < kGradSumWarps) {
         more_registers<kRegsSum>();
@@ -197,58 +231,74 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
                     *reinterpret_cast<float4*>(dst + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
         }
     } else if (warp < kGradBWarp) {
-        more_registers<kRegsA>();
-        const int q = warp & 3;
+        const int q = warp & 3, group = (warp - kGradSumWarps) >> 2;
         const uint32_t column = 4u * (32 * q + lane);
-        for (int c = 0; c < count; ++c) {
+        if (group) advance(hop, in_hop);
+        for (int c = group; c < count; c += 2) {
             const int s = c % kGradStages, r0 = c % kGradRaw;
-            const bool relu = (a.relu_mask >> hop_of(first + c)) & 1u;
+            const bool relu = (a.relu_mask >> hop) & 1u;
+            advance(hop, in_hop);
+            advance(hop, in_hop);
             if (!tc_wait_warp(raw_full(r0), (uint32_t)(c / kGradRaw) & 1u, abort_flag, a.error, a.spin_limit)) break;
-            const uint32_t dy = raw0 + r0 * kGradRawStage + column, y = dy + kGradMatrix;
+            const uint32_t dy = raw0 + r0 * kGradRawStage + column, y = dy + kGradMatrix, rows = rows_of[r0];
             float v[kGradChunk];
 #pragma unroll
             for (int r = 0; r < kGradChunk; ++r) v[r] = grad_read(dy + 4u * kGradTile * r);
             if (relu) {
+                float m[kGradChunk];
 #pragma unroll
-                for (int r = 0; r < kGradChunk; ++r) v[r] = grad_read(y + 4u * kGradTile * r) > 0.f ? v[r] : 0.f;
+                for (int r = 0; r < kGradChunk; ++r) m[r] = grad_read(y + 4u * kGradTile * r);
+#pragma unroll
+                for (int r = 0; r < kGradChunk; ++r) v[r] = m[r] > 0.f ? v[r] : 0.f;
             }
             __syncwarp();
             if (lane == 0) tc_bar_arrive(raw_empty(r0));
-            if (!tc_wait_warp(empty(s), ((uint32_t)(c / kGradStages) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit)) break;
-            tc_fence_after();
-            uint32_t p[3][16];
+            if (rows != kGradAllRows) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+                for (int r = 0; r < kGradChunk; ++r) v[r] = rows >> r & 1u ? v[r] : 0.f;
+            }
+            uint32_t p[3][kGradChunk / 2];
+#pragma unroll
+            for (int j = 0; j < kGradChunk / 2; ++j) {
                 const Parts e = cut(v[2 * j]), o = cut(v[2 * j + 1]);
                 p[0][j] = pack(e.h, o.h);
                 p[1][j] = pack(e.m, o.m);
                 p[2][j] = pack(e.l, o.l);
             }
+            if (!tc_wait_warp(empty(s), ((uint32_t)(c / kGradStages) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit)) break;
+            tc_fence_after();
             const uint32_t to = tmem + ((uint32_t)(32 * q) << 16) + kGradTmemA + kGradTmemStage * s;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) tc_store16(to + 16 * i, p[i]);
+            for (int i = 0; i < 3; ++i) tc_store8(to + kGradChunk / 2 * i, p[i]);
             tc_store_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) tc_bar_arrive(full(s));
         }
     } else if (warp < kGradCopyWarp) {
-        const int w = warp - kGradBWarp, col = 4 * lane;  // of the tile
+        fewer_registers<kRegsB>();
         constexpr int kRows = kGradChunk / 4;
-        for (int c = 0; c < count; ++c) {
+        const int col = 4 * lane, first_row = (warp & 3) * kRows, group = (warp - kGradBWarp) >> 2;  // of the tile, of the chunk
+        for (int c = group; c < count; c += 2) {
             const int s = c % kGradStages, r0 = c % kGradRaw;
             if (!tc_wait_warp(raw_full(r0), (uint32_t)(c / kGradRaw) & 1u, abort_flag, a.error, a.spin_limit)) break;
-            const uint32_t from = raw0 + r0 * kGradRawStage + 2 * kGradMatrix + 16u * lane;
+            const uint32_t from = raw0 + r0 * kGradRawStage + 2 * kGradMatrix + 16u * lane + 4u * kGradTile * first_row;
+            const uint32_t rows = rows_of[r0];
             float4 v[kRows];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) v[i] = grad_read4(from + 4u * kGradTile * (w * kRows + i));
+            for (int i = 0; i < kRows; ++i) v[i] = grad_read4(from + 4u * kGradTile * i);
             __syncwarp();
             if (lane == 0) tc_bar_arrive(raw_empty(r0));
+            if (rows != kGradAllRows) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+                    if (!(rows >> (first_row + i) & 1u)) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
             if (!tc_wait_warp(empty(s), ((uint32_t)(c / kGradStages) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit)) break;
             const uint32_t to = base + (uint32_t)s * kGradStage + (col / 64) * (kGradChunk * 128) + (col % 8) * 2;
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                const int k = w * kRows + i;
+                const int k = first_row + i;
                 const Parts x = cut(v[i].x), y = cut(v[i].y), z = cut(v[i].z), u = cut(v[i].w);
                 const uint32_t at = to + 128u * k + ((uint32_t)((col % 64 / 8) ^ (k & 7)) << 4);
                 asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(pack(x.h, y.h)), "r"(pack(z.h, u.h)) : "memory");
@@ -259,101 +309,135 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
             __syncwarp();
             if (lane == 0) tc_bar_arrive(full(s));
         }
-    } else if (warp < kGradMmaWarp) {
-        fewer_registers<kRegsCopy>();
-        const int w = warp - kGradCopyWarp;
-        constexpr int kRows = kGradChunk / 4;
-        const int col = 4 * lane;  // of the tile
-        const int left = col < a.width ? a.feat_dim - f0 - col : 0;  // features from here on
-        const bool column = h0 + col < a.hidden;                     // (hidden is a multiple of 16)
-        // the hop matrix's row of this lane's row of a chunk; -1: there is none
-        auto row_index = [&](int64_t chunk) {
-            const int64_t pos = (chunk - hop_of(chunk) * a.chunks_per_hop) * kGradChunk + lane;
-            if (pos >= a.batch_size) return -1;
-            const int64_t r = a.batch ? (int64_t)__ldg(a.batch + pos) : pos;
-            return r >= 0 && r < a.n ? (int)r : -1;
-        };
-        int row = count > 0 ? row_index(first) : -1;
-        for (int c = 0; c < count; ++c) {
-            const int next = c + 1 < count ? row_index(first + c + 1) : -1;  // a chunk ahead
-            const int64_t chunk = first + c;
-            const int hop = hop_of(chunk), r0 = c % kGradRaw;
-            const int64_t row0 = (chunk - hop * a.chunks_per_hop) * kGradChunk + w * kRows;
-            const bool relu = (a.relu_mask >> hop) & 1u;
-            if (!tc_wait_warp(raw_empty(r0), ((uint32_t)(c / kGradRaw) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit)) break;
-            const uint32_t to = raw0 + r0 * kGradRawStage + 4u * kGradTile * (w * kRows);
-            const float* x = a.hop[hop] + f0 + col;
-            auto copy_rows = [&](uint32_t dst, const float* src, int64_t ld) {
-                if (a.wide) {
-                    src += h0 + col;
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const bool there = __shfl_sync(0xffffffffu, row, w * kRows + i) >= 0, live = there && column;
-                        grad_copy<16>(dst + 4u * kGradTile * i + 16u * lane, live ? src + i * ld : a.dy, live);
-                    }
-                } else {
-                    src += h0 + lane;
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const bool there = __shfl_sync(0xffffffffu, row, w * kRows + i) >= 0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const bool live = there && h0 + 32 * j + lane < a.hidden;
-                            grad_copy<4>(dst + 4u * kGradTile * i + 128u * j + 4u * lane, live ? src + i * ld + 32 * j : a.dy, live);
-                        }
-                    }
-                }
-            };
-            copy_rows(to, a.dy + hop * a.dy_hop + row0 * a.lddy, a.lddy);
-            if (relu) copy_rows(to + kGradMatrix, a.y + hop * a.y_hop + row0 * a.ldy, a.ldy);
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int r = __shfl_sync(0xffffffffu, row, w * kRows + i);
-                const uint32_t dst = to + 2 * kGradMatrix + 4u * kGradTile * i + 16u * lane;
-                const float* src = x + (int64_t)max(r, 0) * a.ldh;
-                if (left >= 4 || left <= 0) {
-                    grad_copy<16>(dst, left > 0 && r >= 0 ? src : a.hop[hop], left > 0 && r >= 0);
-                } else {  // the last features, without what lies behind them
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) grad_copy<4>(dst + 4u * j, j < left && r >= 0 ? src + j : a.hop[hop], j < left && r >= 0);
-                }
-            }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(raw_full(r0)) : "memory");
-            row = next;
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");  // nothing may land after this CTA has left
     } else {
-        fewer_registers<kRegsMma>();
-        if (warp == kGradMmaWarp) {
-            const uint32_t instr = tc_instr(kGradTile, a.width, true, true);
-            bool ok = true;
-            for (int i = 0, c = 0; i < slices && ok; ++i) {
-                ok = tc_wait_warp(acc_empty(i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
-                for (const int start = c; ok && c < min(start + kGradSlice, count); ++c) {
-                    const int s = c % kGradStages;
-                    ok = tc_wait_warp(full(s), (uint32_t)(c / kGradStages) & 1u, abort_flag, a.error, a.spin_limit);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t d = tmem + (uint32_t)(i & 1) * kGradTile, am = tmem + kGradTmemA + kGradTmemStage * s;
-                    const uint32_t at = base + (uint32_t)s * kGradStage;
-                    const uint64_t b[3] = {tc_desc_mn(at, kGradChunk * 128), tc_desc_mn(at + kGradPart, kGradChunk * 128),
-                                           tc_desc_mn(at + 2 * kGradPart, kGradChunk * 128)};
-                    // the small terms first
-                    constexpr int kA[6] = {1, 2, 0, 1, 0, 0}, kB[6] = {1, 0, 2, 0, 1, 0};
-#pragma unroll
-                    for (int t = 0; t < 6; ++t)
-#pragma unroll
-                        for (int j = 0; j < kGradChunk / 16; ++j)
-                            tc_mma_ta(d, am + 16 * kA[t] + 8 * j, b[kB[t]] + (2048 >> 4) * j, instr, c != start || t != 0 || j != 0);
-                    tc_commit(empty(s));
-                }
-                if (ok) tc_commit(acc_full(i & 1));
-            }
-            tc_commit(drained);
+        fewer_registers<kRegsRest>();
+    }
+    // nothing may land after this CTA has left: the last copies of the ring's places t, t + step, ...
+    auto landed = [&](int issued, int t, int step) {
+        for (; t < min(issued, kGradRaw); t += step)
             for (uint32_t i = 0; i < kTcSpinLimit; ++i)
-                if (tc_bar_test(drained, 0)) break;
-            __syncwarp();
+                if (tc_bar_test(raw_full(t), (uint32_t)((issued - t + kGradRaw - 1) / kGradRaw - 1) & 1u)) break;
+    };
+    if (warp == kGradCopyWarp || warp == kGradCopyWarp + 1) {
+        static_assert(kGradRaw % 2 == 0, "the warps take places in turn");
+        const int w = warp - kGradCopyWarp, n = (int)a.n, rows_in = (int)a.batch_size;
+        // This lane's row of the hop matrix in a chunk, -1 or another row outside for none.  Asked for kAhead of the warp's chunks
+        // ahead: with one, copies were issued no faster than one load from memory after the other.
+        constexpr int kAhead = 4;
+        auto ask = [&](int c) {
+            const int64_t pos = (int64_t)c * kGradChunk + lane;
+            if (lane >= kGradChunk || pos >= rows_in) return -1;
+            return a.batch ? __ldg(a.batch + pos) : (int)pos;
+        };
+        if (w == 1) advance(hop, in_hop);
+        int asked[kAhead], ask_hop = hop, ask_in = in_hop;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            asked[j] = w + 2 * j < count ? ask(ask_in) : -1;
+            advance(ask_hop, ask_in);
+            advance(ask_hop, ask_in);
         }
+        const int first4 = 4 * (lane & (kGradChunk / 4 - 1));
+        int place = w, issued = 0;  // issued: chunks up to this warp's last
+        uint32_t ph = 1;
+        bool ok = true;
+        for (int c0 = w; c0 < count && ok; c0 += 2 * kAhead)
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int c = c0 + 2 * j, row = asked[j];
+                if (c >= count || !ok) continue;
+                if (c + 2 * kAhead < count) asked[j] = ask(ask_in);
+                advance(ask_hop, ask_in);
+                advance(ask_hop, ask_in);
+                // (rows that do not exist are fetched from row 0 and left out when the chunk is split)
+                const bool exists = row >= 0 && row < n;
+                const uint32_t rows = __ballot_sync(0xffffffffu, exists);
+                const int from = exists ? row : 0;
+                const int q0 = __shfl_sync(0xffffffffu, from, first4), q1 = __shfl_sync(0xffffffffu, from, first4 + 1),
+                          q2 = __shfl_sync(0xffffffffu, from, first4 + 2), q3 = __shfl_sync(0xffffffffu, from, first4 + 3);
+                ok = tc_wait_warp(raw_empty(place), ph, abort_flag, a.error, a.spin_limit);
+                if (!ok) continue;
+                const uint32_t to = raw0 + place * kGradRawStage, bar = raw_full(place);
+                if (lane == 0) {
+                    rows_of[place] = rows;
+                    tc_bar_expect(bar, kGradMatrix);
+                }
+                __syncwarp();
+                if (lane < kGradChunk / 4) grad_gather4(to + 2 * kGradMatrix + 4u * kGradTile * first4, &maps.x[hop], f0, q0, q1, q2, q3, bar);
+                if (!a.wide) {
+                    const int row0 = in_hop * kGradChunk;
+                    auto copy_rows = [&](uint32_t dst, const float* src, int64_t ld) {
+                        for (int i = 0; i < kGradChunk; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const bool live = row0 + i < rows_in && h0 + 32 * k + lane < a.hidden;
+                                grad_copy(dst + 4u * kGradTile * i + 128u * k + 4u * lane, live ? src + (int64_t)(row0 + i) * ld + h0 + 32 * k + lane : a.dy, live);
+                            }
+                    };
+                    copy_rows(to, a.dy + hop * a.dy_hop, a.lddy);
+                    if (a.relu_mask >> hop & 1u) copy_rows(to + kGradMatrix, a.y + hop * a.y_hop, a.ldy);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                }
+                advance(hop, in_hop);
+                advance(hop, in_hop);
+                issued = c + 1;
+                place += 2;
+                if (place >= kGradRaw) {
+                    place -= kGradRaw;
+                    ph ^= 1u;
+                }
+            }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        landed(issued, w, 2);
+    } else if (warp == kGradTileWarp) {
+        if (lane == 0 && a.wide) {
+            int place = 0, issued = 0;
+            uint32_t ph = 1;
+            for (; issued < count; ++issued) {
+                if (!tc_wait(raw_empty(place), ph, abort_flag, a.error, a.spin_limit)) break;
+                const bool relu = a.relu_mask >> hop & 1u;
+                const uint32_t to = raw0 + place * kGradRawStage, bar = raw_full(place);
+                tc_bar_expect(bar, kGradMatrix * (1 + relu));
+                grad_tile(to, &maps.dy, h0, in_hop * kGradChunk, hop, bar);
+                if (relu) grad_tile(to + kGradMatrix, &maps.y, h0, in_hop * kGradChunk, hop, bar);
+                advance(hop, in_hop);
+                if (++place == kGradRaw) {
+                    place = 0;
+                    ph ^= 1u;
+                }
+            }
+            landed(issued, 0, 1);
+        }
+        __syncwarp();
+    } else if (warp == kGradMmaWarp) {
+        const uint32_t instr = tc_instr(kGradTile, a.width, true, true);
+        bool ok = true;
+        for (int i = 0, c = 0; i < slices && ok; ++i) {
+            ok = tc_wait_warp(acc_empty(i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
+            for (const int start = c; ok && c < min(start + kGradSlice, count); ++c) {
+                const int s = c % kGradStages;
+                ok = tc_wait_warp(full(s), (uint32_t)(c / kGradStages) & 1u, abort_flag, a.error, a.spin_limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(i & 1) * kGradTile, am = tmem + kGradTmemA + kGradTmemStage * s;
+                const uint32_t at = base + (uint32_t)s * kGradStage;
+                const uint64_t b[3] = {tc_desc_mn(at, kGradChunk * 128), tc_desc_mn(at + kGradPart, kGradChunk * 128),
+                                       tc_desc_mn(at + 2 * kGradPart, kGradChunk * 128)};
+                // the small terms first
+                constexpr int kA[6] = {1, 2, 0, 1, 0, 0}, kB[6] = {1, 0, 2, 0, 1, 0};
+#pragma unroll
+                for (int t = 0; t < 6; ++t)
+#pragma unroll
+                    for (int j = 0; j < kGradChunk / 16; ++j)
+                        tc_mma_ta(d, am + kGradChunk / 2 * kA[t] + 8 * j, b[kB[t]] + (2048 >> 4) * j, instr, c != start || t != 0 || j != 0);
+                tc_commit(empty(s));
+            }
+            if (ok) tc_commit(acc_full(i & 1));
+        }
+        tc_commit(drained);
+        for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+            if (tc_bar_test(drained, 0)) break;
+        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
@@ -420,6 +504,31 @@ GradShape grad_shape(int64_t num_hops, int64_t batch_size, int64_t feat_dim, int
     return g;
 }
 
+int encode_map(const float* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, CUtensorMap* out) {
+    typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+    static std::atomic<encode_fn> cached{nullptr};  // threads may race to fill it; they all store the same pointer
+    encode_fn encode = cached.load(std::memory_order_acquire);
+    if (!encode) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        GNNPRE_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q));
+        if (q != cudaDriverEntryPointSuccess || !fn) return GNNPRE_ERR_CUDA;
+        encode = reinterpret_cast<encode_fn>(fn);
+        cached.store(encode, std::memory_order_release);
+    }
+    const cuuint32_t elem[3] = {1u, 1u, 1u};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (cuuint32_t)rank, const_cast<float*>(base), dims, strides, box, elem,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_last_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled", __FILE__, __LINE__);
+        return GNNPRE_ERR_CUDA;
+    }
+    return GNNPRE_OK;
+}
+
 // More than any device of this architecture has, for a size that does not depend on the device.
 constexpr int kMostSms = 192;
 
@@ -470,6 +579,10 @@ int grad_launch(const float* const* hops, int32_t num_hops, int64_t n, int64_t f
         if (accumulate) return GNNPRE_OK;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const auto join = [&](int32_t splits, bool add, bool after) {
+        return launch_after(k_lc_grad_join, dim3((unsigned)((feat_dim + 127) / 128), (unsigned)hidden), 32 * kJoinGroups, 0, after, st,
+                            (const float*)workspace, g.part_ld, splits, (int32_t)hidden, (int32_t)feat_dim, (int32_t)add, dWt, ldw);
+    };
     if (!empty) {
         static std::atomic<bool> opted_in[kMaxDevices];
         int dev = 0;
@@ -479,39 +592,58 @@ int grad_launch(const float* const* hops, int32_t num_hops, int64_t n, int64_t f
             if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
         }
         GradArgs a{};
-        for (int32_t k = 0; k < num_hops; ++k) a.hop[k] = hops[k];
-        a.ldh = ldh;
         a.n = n;
         a.feat_dim = (int32_t)feat_dim;
         a.hidden = (int32_t)hidden;
-        a.num_hops = num_hops;
         a.batch = batch;
         a.batch_size = batch_size;
-        a.dy = dY;
         a.lddy = lddy;
         a.dy_hop = dy_hop;
-        a.y = Y;
         a.ldy = ldy;
         a.y_hop = y_hop;
-        a.relu_mask = used;
         a.tiles_f = g.tiles_f;
         a.width = g.width;
         a.tiles = g.tiles;
-        a.splits = g.splits;
-        a.chunks_per_hop = g.chunks_per_hop;
-        a.chunks = g.chunks;
+        a.chunks_per_hop = (int32_t)g.chunks_per_hop;
         a.parts = static_cast<float*>(workspace);
         a.part_ld = g.part_ld;
         a.error = error_flag;
         a.spin_limit = polls;
         a.drop = drop;
-        a.wide = ((reinterpret_cast<uintptr_t>(dY) | (uintptr_t)(lddy * 4) | (uintptr_t)(dy_hop * 4)) % 16 == 0) &&
-                 (!used || (reinterpret_cast<uintptr_t>(Y) | (uintptr_t)(ldy * 4) | (uintptr_t)(y_hop * 4)) % 16 == 0);
-        k_lc_grad<<<(unsigned)((int64_t)g.tiles * g.splits), kGradThreads, kGradSmem, st>>>(a);
-        GNNPRE_CUDA(cudaGetLastError());
+        for (int32_t k0 = 0; k0 < num_hops; k0 += kGradMaxHops) {  // further hops are added to the first ones' sum
+            const int32_t kn = std::min(kGradMaxHops, num_hops - k0);
+            const GradShape now = grad_shape(kn, batch_size, feat_dim, hidden, std::min(sms, kMostSms));
+            a.relu_mask = used >> k0 & ((1ull << kn) - 1);
+            a.dy = dY + k0 * dy_hop;
+            a.y = a.relu_mask ? Y + k0 * y_hop : nullptr;
+            a.splits = now.splits;
+            a.chunks = now.chunks;
+            const auto tiled = [&](const float* p, int64_t ld, int64_t hop) {
+                return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 4)) % 16 == 0 && ld < ((int64_t)1 << 36) &&
+                       (kn == 1 || (hop > 0 && hop % 4 == 0 && hop < ((int64_t)1 << 36)));
+            };
+            a.wide = tiled(a.dy, lddy, dy_hop) && (!a.relu_mask || tiled(a.y, ldy, y_hop));
+            GradMaps maps{};
+            for (int32_t k = 0; k < kn; ++k) {
+                const cuuint64_t dims[2] = {(cuuint64_t)feat_dim, (cuuint64_t)n}, strides[1] = {(cuuint64_t)ldh * 4};
+                const cuuint32_t box[2] = {kGradTile, 1u};
+                GNNPRE_TRY(encode_map(hops[k0 + k], 2, dims, strides, box, &maps.x[k]));
+            }
+            if (a.wide) {
+                const cuuint64_t dims[3] = {(cuuint64_t)hidden, (cuuint64_t)batch_size, (cuuint64_t)kn};
+                const cuuint32_t box[3] = {kGradTile, kGradChunk, 1u};
+                const cuuint64_t dy_strides[2] = {(cuuint64_t)lddy * 4, kn > 1 ? (cuuint64_t)dy_hop * 4 : (cuuint64_t)16};
+                GNNPRE_TRY(encode_map(a.dy, 3, dims, dy_strides, box, &maps.dy));
+                const cuuint64_t y_strides[2] = {(cuuint64_t)ldy * 4, kn > 1 ? (cuuint64_t)y_hop * 4 : (cuuint64_t)16};
+                if (a.relu_mask) GNNPRE_TRY(encode_map(a.y, 3, dims, y_strides, box, &maps.y));
+            }
+            k_lc_grad<<<(unsigned)((int64_t)g.tiles * now.splits), kGradThreads, kGradSmem, st>>>(maps, a);
+            GNNPRE_CUDA(cudaGetLastError());
+            GNNPRE_TRY(join(now.splits, accumulate || k0 > 0, true));
+        }
+        return GNNPRE_OK;
     }
-    return launch_after(k_lc_grad_join, dim3((unsigned)((feat_dim + 127) / 128), (unsigned)hidden), 32 * kJoinGroups, 0, !empty, st,
-                        (const float*)workspace, g.part_ld, g.splits, (int32_t)hidden, (int32_t)feat_dim, (int32_t)(accumulate != 0), dWt, ldw);
+    return join(0, false, false);
 }
 
 }  // namespace
