@@ -433,6 +433,674 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
     }
 }
 
+// ------------------------------------------------------------------------------------------------ small matrices, one launch
+
+// All of it for one matrix by one cluster of CTAs, which share out the tiles of each product, exchange them through the L2 and wait
+// for one another between products (three per step).  A product by itself takes some 7.5 us as a launch of its own: its CTAs
+// start, set up barriers and tensor memory, wait for the first copies, and leave.
+struct Steps {
+    float gram[kMaxSteps];                                   // alpha of A = X X^T
+    float p[kMaxSteps], p_a[kMaxSteps], p_diag[kMaxSteps];   // alpha, beta and diag of P
+    float apply[kMaxSteps];                                  // alpha of X = P X
+};
+
+struct Cluster {
+    Source src;
+    Split a, p, xt[2];   // (x and xt[0] are the source's)
+    int32_t rp, np, k_r, k_n, steps;
+    void* out;
+    int64_t ldo, out_batch;
+    float out_factor;
+    int32_t* error;
+    uint32_t spin_limit;
+    int32_t drop;
+    Steps s;
+};
+
+constexpr int kClusterTile = 64;                                         // columns of a tile
+constexpr uint32_t kClusterStage = kBlockBytes + kClusterTile * 128 * 2; // a chunk of A's 128 rows and B's 64
+constexpr int kClusterStages = 3;
+constexpr int kClusterStaging = 2 * kBlockBytes;                         // a tile and its transpose
+constexpr int kClusterSmem = kClusterStages * (int)kClusterStage + kClusterStaging + 1024;
+constexpr int kClusterSourceTiles = (kClusterSmem - 1024) / (64 * 65 * 4);
+constexpr int kMostClusterTiles = 48;   // tiles of X in a product, at most
+static_assert(2 * kMostClusterTiles / 8 <= kClusterSourceTiles, "the [64, 64] tiles of X that a CTA reads fit");
+
+__device__ __forceinline__ void ns_cluster_sync() {
+    // what either proxy has written is seen by either proxy of the others
+    asm volatile("fence.proxy.async;" ::: "memory");
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+__device__ __forceinline__ void ns_sum_warps_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+__global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_constant__ Cluster a) {
+    constexpr int BN = kClusterTile, kCols = BN / 2;
+    constexpr uint32_t kBBytes = BN * 128;
+    extern __shared__ unsigned char ns_smem[];
+    __shared__ __align__(8) unsigned long long bars[2 * kClusterStages + 5];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    __shared__ double room[kProductThreads / 32];
+    volatile int* abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank, ctas;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+    const int64_t batch = blockIdx.x / ctas;
+    const uint32_t base = (tc_smem(ns_smem) + 1023u) & ~1023u;
+    unsigned char* const base_p = ns_smem + (base - tc_smem(ns_smem));
+    const uint32_t bar0 = tc_smem(&bars[0]);
+    auto full = [&](int s) { return bar0 + 8u * s; };
+    auto empty = [&](int s) { return bar0 + 8u * (kClusterStages + s); };
+    auto acc_full = [&](int b) { return bar0 + 8u * (2 * kClusterStages + b); };
+    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kClusterStages + 2 + b); };
+    const uint32_t drained = bar0 + 8u * (2 * kClusterStages + 4);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kClusterStages; ++s) {
+            tc_bar_init(full(s), 1 + (a.drop ? 1 : 0));
+            tc_bar_init(empty(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc_bar_init(acc_full(b), 1);
+            tc_bar_init(acc_empty(b), kSumWarps);
+        }
+        tc_bar_init(drained, 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), 2 * BN);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    // G, read once: this CTA's [64, 64] tiles of X go to shared memory, their squares to the norm
+    const Source& src = a.src;
+    const int side_tiles = a.np / 64, tiles = side_tiles * (a.rp / 64);
+    float(*const tile)[64][65] = reinterpret_cast<float(*)[64][65]>(base_p);
+    double sum2 = 0;
+    for (int t = rank, k = 0; t < tiles; t += ctas, ++k) {
+        const int i0 = t / side_tiles * 64, j0 = t % side_tiles * 64, fast = threadIdx.x & 63;
+        if (warp >= kSumWarps) continue;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const int slow = (threadIdx.x >> 6) + 4 * u;
+            const int gi = (src.tall ? j0 : i0) + slow, gj = (src.tall ? i0 : j0) + fast;
+            const float v = gi < src.rows && gj < src.cols ? source_at(src, batch, gi, gj) : 0.f;
+            tile[k][src.tall ? fast : slow][src.tall ? slow : fast] = v;
+            sum2 += (double)v * v;
+        }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) sum2 += __shfl_xor_sync(0xffffffffu, sum2, d);
+    if (lane == 0) room[warp] = sum2;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kSumWarps; ++w) sum2 += room[w];
+        src.partial[batch * kNormBlocks + rank] = sum2;
+    }
+    ns_cluster_sync();
+    if (threadIdx.x < 32) {  // the CTAs' sums, in their order
+        double v = lane < (int)ctas ? __ldcg(src.partial + batch * kNormBlocks + lane) : 0.0, total = 0;
+        for (int c = 0; c < (int)ctas; ++c) total += __shfl_sync(0xffffffffu, v, c);
+        if (lane == 0) room[0] = 1.0 / (sqrt(total) + src.eps) * (double)src.factor;
+    }
+    __syncthreads();
+    const double scale = room[0];
+    for (int t = rank, k = 0; t < tiles; t += ctas, ++k) {
+        const int i0 = t / side_tiles * 64, j0 = t % side_tiles * 64;
+        for (int c = threadIdx.x; c < 64 * 8; c += kProductThreads) {
+            const int row = c >> 3, chunk = c & 7;
+            float v[8];
+            uint4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)((double)tile[k][row][8 * chunk + e] * scale);
+            split8(v, hi, lo);
+            unsigned char* d = src.x.block(batch, (i0 + row) / kBlockRows, j0 / kBlockCols) + block_byte((i0 + row) % kBlockRows, 8 * chunk);
+            *reinterpret_cast<uint4*>(d) = hi;
+            *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)((double)tile[k][8 * chunk + e][row] * scale);
+            split8(v, hi, lo);
+            d = src.xt.block(batch, (j0 + row) / kBlockRows, i0 / kBlockCols) + block_byte((j0 + row) % kBlockRows, 8 * chunk);
+            *reinterpret_cast<uint4*>(d) = hi;
+            *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+        }
+    }
+    ns_cluster_sync();
+
+    // chunks copied or multiplied, accumulators filled or added up so far: each role counts for itself
+    int chunk = 0, issued = 0;
+    bool ok = true;
+    const uint32_t instr = tc_instr(kBlockRows, BN, false);
+    unsigned char* const staging_p = base_p + kClusterStages * kClusterStage;
+    const uint32_t staging = base + kClusterStages * kClusterStage;
+    bool stored = false;
+    for (int stage = 0; stage < 3 * a.steps; ++stage) {
+        const int step = stage / 3, kind = stage % 3;
+        const bool last = stage == 3 * a.steps - 1, tall = last && src.tall;
+        const Split& xt = a.xt[step & 1];
+        const Split& sa = kind == 0 ? src.x : kind == 1 ? a.a : tall ? xt : a.p;
+        const Split& sb = kind == 0 ? src.x : kind == 1 ? a.a : tall ? a.p : xt;
+        const int rows = tall ? a.np : a.rp, cols = kind < 2 || tall ? a.rp : a.np;
+        const int k_chunks = kind == 0 ? a.k_n : a.k_r, tiles_n = cols / BN, all = rows / kBlockRows * tiles_n;
+        for (int t = rank; t < all; t += ctas) {
+            const int bi = t / tiles_n, bj = t % tiles_n;
+            if (warp < kSumWarps) {
+                float sum[kCols];
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
+                const int q = warp & 3, half = warp >> 2, row = 32 * q + lane;
+                for (int i = 0; i < k_chunks; ++i, ++chunk) {
+                    ok = ok && tc_wait_warp(acc_full(chunk & 1), (uint32_t)(chunk >> 1) & 1u, abort_flag, a.error, a.spin_limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t v[32];
+                    tc_load32(tmem + ((uint32_t)(32 * q) << 16) + half * kCols + (uint32_t)(chunk & 1) * BN, v);
+                    tc_load_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[j] += __uint_as_float(v[j]);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc_bar_arrive(acc_empty(chunk & 1));
+                }
+                if (last) {
+                    if (!ok) continue;
+                    float* line = reinterpret_cast<float*>(staging_p) + warp * (32 * 33);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[j] * a.out_factor;
+                    __syncwarp();
+                    const int col = bj * BN + half * kCols + lane;
+                    if (col < src.cols)
+                        for (int r = 0; r < 32; ++r) {
+                            const int64_t i = (int64_t)bi * kBlockRows + 32 * q + r;
+                            if (i >= src.rows) break;
+                            const int64_t at = batch * a.out_batch + i * a.ldo + col;
+                            const float o = line[r * 33 + lane];
+                            if (src.dtype == GNNPRE_F32) static_cast<float*>(a.out)[at] = o;
+                            else if (src.dtype == GNNPRE_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(o);
+                            else static_cast<__half*>(a.out)[at] = __float2half_rn(o);
+                        }
+                    __syncwarp();
+                    continue;
+                }
+                const float alpha = kind == 0 ? a.s.gram[step] : kind == 1 ? a.s.p[step] : a.s.apply[step];
+                const float beta = a.s.p_a[step], on_diag = a.s.p_diag[step];
+                const int c0 = half * kCols, col0 = bj * BN + c0, diag = bi * kBlockRows + row - col0;
+                uint4 ch[4], cl[4];
+                if (kind == 1) {
+                    const unsigned char* c = a.a.block(batch, bi, col0 / kBlockCols);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        ch[j] = __ldcg(reinterpret_cast<const uint4*>(c + block_byte(row, col0 % kBlockCols + 8 * j)));
+                        cl[j] = __ldcg(reinterpret_cast<const uint4*>(c + kHalfBytes + block_byte(row, col0 % kBlockCols + 8 * j)));
+                    }
+                }
+                // the staging is free when the last tile's copies have read it
+                if (threadIdx.x == 0 && stored) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                ns_sum_warps_sync();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = alpha * sum[8 * j + e];
+                    if (kind == 1) {
+                        const __half2* h = reinterpret_cast<const __half2*>(&ch[j]);
+                        const __half2* l = reinterpret_cast<const __half2*>(&cl[j]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 fh = __half22float2(h[e]), fl = __half22float2(l[e]);
+                            o[2 * e] = fmaf(beta, fh.x + fl.x, o[2 * e]);
+                            o[2 * e + 1] = fmaf(beta, fh.y + fl.y, o[2 * e + 1]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (8 * j + e == diag) o[e] += on_diag;
+                    }
+                    uint4 hi, lo;
+                    split8(o, hi, lo);
+                    unsigned char* d = staging_p + block_byte(row, c0 + 8 * j);
+                    *reinterpret_cast<uint4*>(d) = hi;
+                    *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+                    if (kind == 2) {
+                        const __half* h = reinterpret_cast<const __half*>(&hi);
+                        const __half* l = reinterpret_cast<const __half*>(&lo);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            unsigned char* u = staging_p + kBlockBytes + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
+                            *reinterpret_cast<__half*>(u) = h[e];
+                            *reinterpret_cast<__half*>(u + kBBytes) = l[e];
+                        }
+                    }
+                }
+                tc_fence_async();
+                ns_sum_warps_sync();
+                if (threadIdx.x == 0) {
+                    const Split& to = kind == 0 ? a.a : kind == 1 ? a.p : src.x;
+                    tc_bulk_store(to.block(batch, bi, bj), staging, kBlockBytes);
+                    if (kind == 2) {
+                        const int rows0 = bj * BN % kBlockRows;
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            unsigned char* u = a.xt[(step & 1) ^ 1].block(batch, bj * BN / kBlockRows, 2 * bi + b) + rows0 * 128;
+                            tc_bulk_store(u, staging + kBlockBytes + b * 2 * kBBytes, kBBytes);
+                            tc_bulk_store(u + kHalfBytes, staging + kBlockBytes + b * 2 * kBBytes + kBBytes, kBBytes);
+                        }
+                    }
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    stored = true;
+                }
+            } else if (warp == kCopyWarp) {
+                if (lane == 0) {
+                    const int rows0 = bj * BN % kBlockRows, rb = bj * BN / kBlockRows;
+                    for (int kc = 0; kc < k_chunks && ok; ++kc) {
+                        const int s = chunk % kClusterStages;
+                        ok = tc_wait(empty(s), ((uint32_t)(chunk / kClusterStages) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
+                        if (!ok) break;
+                        const uint32_t to = base + (uint32_t)s * kClusterStage;
+                        const unsigned char* b = sb.block(batch, rb, kc);
+                        tc_bar_expect(full(s), kClusterStage);
+                        tc_bulk_load(to, sa.block(batch, bi, kc), kBlockBytes, full(s));
+                        tc_bulk_load(to + kBlockBytes, b + rows0 * 128, kBBytes, full(s));
+                        tc_bulk_load(to + kBlockBytes + kBBytes, b + kHalfBytes + rows0 * 128, kBBytes, full(s));
+                        ++chunk;
+                        ++issued;
+                    }
+                }
+                __syncwarp();
+            } else {
+                for (int kc = 0; kc < k_chunks && ok; ++kc) {
+                    const int s = chunk % kClusterStages;
+                    ok = tc_wait_warp(acc_empty(chunk & 1), ((uint32_t)(chunk >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit) &&
+                         tc_wait_warp(full(s), (uint32_t)(chunk / kClusterStages) & 1u, abort_flag, a.error, a.spin_limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = base + (uint32_t)s * kClusterStage, d = tmem + (uint32_t)(chunk & 1) * BN;
+                    const uint64_t ah = tc_desc_k(at), al = tc_desc_k(at + kHalfBytes), bh = tc_desc_k(at + kBlockBytes),
+                                   bl = tc_desc_k(at + kBlockBytes + kBBytes);
+#pragma unroll
+                    for (int j = 0; j < kBlockCols / 16; ++j) {
+                        tc_mma(d, al + 2 * j, bh + 2 * j, instr, j != 0);
+                        tc_mma(d, ah + 2 * j, bl + 2 * j, instr, 1u);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(d, ah + 2 * j, bh + 2 * j, instr, 1u);
+                    tc_commit(empty(s));
+                    tc_commit(acc_full(chunk & 1));
+                    ++chunk;
+                }
+            }
+        }
+        if (!last) {
+            if (threadIdx.x == 0 && stored) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            ns_cluster_sync();  // (given up or not: every CTA comes here as often)
+        }
+    }
+    if (warp == kCopyWarp && lane == 0) {
+        // every copy has landed before this CTA leaves (a self-test's barriers: see k_ns_product)
+        if (a.drop) {
+            for (uint32_t i = 0; i < 4 * a.spin_limit && !*abort_flag; ++i) __nanosleep(kTcSuspendNs);
+            *abort_flag = 1;
+        }
+        for (int t = 0; t < min(issued, kClusterStages); ++t) {
+            if (a.drop) tc_bar_arrive(full(t));
+            for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+                if (tc_bar_test(full(t), (uint32_t)((issued - t + kClusterStages - 1) / kClusterStages - 1) & 1u)) break;
+        }
+    }
+    if (warp == kMmaWarp) {
+        tc_commit(drained);
+        for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+            if (tc_bar_test(drained, 0)) break;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tc_free(tmem, 2 * BN);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ r <= 128: on the chip
+
+// With r <= 128 all r x r matrices are one tile, and X (or, of a long one, a CTA's share of its columns) stays in shared memory
+// from the first step to the last.  It serves A = X X^T as both operands, rows along K, and P X as operand B as it lies: a row
+// of X is a row along K there (MN-major).  The CTAs of a cluster add up their shares' A, in the order of their ranks, and each
+// computes P for itself.  The eight warps read the accumulators: warps w and w + 4 share lanes 32 (w & 3) .., a half of the
+// columns each; A stays in their registers for P.  As each K-chunk's large terms have an accumulator of their own, four cuts of the
+// tensor core meet in a sum.
+constexpr int kChipThreads = 256;
+constexpr int kChipCols = 256;                       // columns of X in a CTA
+constexpr int kChipMaxCtas = 8;
+constexpr int kChipSmem = (kChipCols / kBlockCols + 2) * kBlockBytes + 1024;
+
+struct Chip {
+    Source src;          // (x, xt: unused)
+    int32_t cols;        // of X per CTA, a multiple of 64
+    int32_t steps;
+    void* out;
+    int64_t ldo, out_batch;
+    float out_factor;
+    int32_t* error;
+    uint32_t spin_limit;
+    int32_t drop;
+    Steps s;
+};
+
+__device__ __forceinline__ float4 ns_read_peer(uint32_t addr, uint32_t rank) {
+    float4 v;
+    asm volatile(
+        "{\n\t.reg .b32 remote;\n\t"
+        "mapa.shared::cluster.u32 remote, %4, %5;\n\t"
+        "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [remote];\n\t}"
+        : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+        : "r"(addr), "r"(rank)
+        : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_constant__ Chip a) {
+    extern __shared__ unsigned char ns_smem[];
+    __shared__ __align__(8) unsigned long long bars[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    __shared__ double room[kChipThreads / 32], norm;
+    volatile int* abort_flag = &abort_word;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank, ctas;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+    const int64_t batch = blockIdx.x / ctas;
+    const uint32_t base = (tc_smem(ns_smem) + 1023u) & ~1023u;
+    unsigned char* const base_p = ns_smem + (base - tc_smem(ns_smem));
+    const uint32_t xs = base, as = base + kChipCols / kBlockCols * kBlockBytes;       // X's blocks; A's, later P's two
+    unsigned char* const as_p = base_p + kChipCols / kBlockCols * kBlockBytes;
+    const uint32_t done = tc_smem(&bars[0]), drained = tc_smem(&bars[1]);
+    if (threadIdx.x == 0) {
+        tc_bar_init(done, 1);
+        tc_bar_init(drained, 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) tc_alloc(tc_smem(&tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const Source& src = a.src;
+    const int r = src.tall ? src.cols : src.rows, n = src.tall ? src.rows : src.cols;
+    const int j0 = (int)rank * a.cols, blocks = a.cols / kBlockCols;
+    const int q = warp & 3, half = warp >> 2, row = 32 * q + lane;
+
+    // This thread's row of X, a half of the share's columns: groups of eight, all read before the norm is known.
+    {
+        constexpr int kGroups = kChipCols / 16;
+        float g[kGroups][8];
+        double sum2 = 0;
+        // (no load depends on a condition, so that all are under way together: what does not exist is read at the matrix's edge)
+        auto load = [&](auto* p) {
+            p += batch * src.batch_stride + (int64_t)min(row, r - 1) * (src.tall ? 1 : src.ldg);
+            const int64_t apart = src.tall ? src.ldg : 1;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[k][e] = to_f32(p[min(j0 + 8 * (2 * k + half) + e, n - 1) * apart]);
+        };
+        if (src.dtype == GNNPRE_F32) load(static_cast<const float*>(src.g));
+        else if (src.dtype == GNNPRE_BF16) load(static_cast<const __nv_bfloat16*>(src.g));
+        else load(static_cast<const __half*>(src.g));
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = 8 * (2 * k + half) + e;
+                if (c >= a.cols || row >= r || j0 + c >= n) g[k][e] = 0.f;
+            }
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum2 += (double)g[k][e] * g[k][e];
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) sum2 += __shfl_xor_sync(0xffffffffu, sum2, d);
+        if (lane == 0) room[warp] = sum2;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < kChipThreads / 32; ++w) sum2 += room[w];
+            if (ctas > 1) src.partial[batch * kNormBlocks + rank] = sum2;
+            else norm = sum2;
+        }
+        if (ctas > 1) {
+            ns_cluster_sync();
+            if (threadIdx.x == 0) {
+                sum2 = 0;
+                for (uint32_t c = 0; c < ctas; ++c) sum2 += __ldcg(src.partial + batch * kNormBlocks + c);
+                norm = sum2;
+            }
+        }
+        __syncthreads();
+        const double scale = 1.0 / (sqrt(norm) + src.eps) * (double)src.factor;
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            const int c = 8 * (2 * k + half);
+            if (c >= a.cols) continue;
+            float v[8];
+            uint4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)((double)g[k][e] * scale);
+            split8(v, hi, lo);
+            unsigned char* d = base_p + c / kBlockCols * kBlockBytes + block_byte(row, c % kBlockCols);
+            *reinterpret_cast<uint4*>(d) = hi;
+            *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+        }
+    }
+
+    bool ok = true;
+    uint32_t ph = 0;
+    const uint32_t square = tc_instr(kBlockRows, 128, false), wide = tc_instr(kBlockRows, a.cols, false, true);
+    // operands written by this CTA's threads, seen by the tensor core
+    auto publish = [&] {
+        tc_fence_async();
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+    };
+    // the products issued since, complete for everybody or given up by everybody
+    auto finish = [&] {
+        if (warp == 0 && !a.drop) tc_commit(done);
+        ok = __syncthreads_and(ok && tc_wait_warp(done, ph, abort_flag, a.error, a.spin_limit));
+        ph ^= 1u;
+        tc_fence_after();
+    };
+    // sums of `accs` accumulators `apart` columns apart, 32 columns from `col`
+    auto read32 = [&](int col, int accs, int apart, float (&sum)[32]) {
+        uint32_t v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[j] = 0.f;
+        for (int k = 0; k < accs; ++k) {
+            tc_load32(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(k * apart + col), v);
+            tc_load_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[j] += __uint_as_float(v[j]);
+        }
+    };
+    // 32 of this thread's numbers to columns col.. of the blocks at p
+    auto write32 = [&](unsigned char* p, int col, const float (&o)[32]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v[8];
+            uint4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = o[8 * j + e];
+            split8(v, hi, lo);
+            unsigned char* d = p + col / kBlockCols * kBlockBytes + block_byte(row, col % kBlockCols + 8 * j);
+            *reinterpret_cast<uint4*>(d) = hi;
+            *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+        }
+    };
+    for (int step = 0; step < a.steps; ++step) {
+        // A = X X^T of this share: the small terms of all chunks and the large ones of the first in one accumulator, those of the
+        // others in one each
+        publish();
+        if (warp == 0 && ok) {
+            for (int b = 0; b < blocks; ++b) {
+                const uint64_t h = tc_desc_k(xs + b * kBlockBytes), l = tc_desc_k(xs + b * kBlockBytes + kHalfBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) {
+                    tc_mma(tmem, l + 2 * j, h + 2 * j, square, b != 0 || j != 0);
+                    tc_mma(tmem, h + 2 * j, l + 2 * j, square, 1u);
+                }
+            }
+            for (int b = 0; b < blocks; ++b) {
+                const uint64_t h = tc_desc_k(xs + b * kBlockBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(tmem + 128 * b, h + 2 * j, h + 2 * j, square, b == 0 || j != 0);
+            }
+        }
+        finish();
+        float av[2][32];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const int col = 64 * half + 32 * part;
+            read32(col, blocks, 128, av[part]);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) av[part][j] *= a.s.gram[step];
+        }
+        if (ctas > 1) {
+            // the shares' sums, laid down where A will be: rows of 32 pieces of 16 bytes, turned by the row
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int piece = (16 * half + 8 * part + j) ^ (row & 31);
+                    *reinterpret_cast<float4*>(as_p + row * 512 + piece * 16) =
+                        make_float4(av[part][4 * j], av[part][4 * j + 1], av[part][4 * j + 2], av[part][4 * j + 3]);
+                }
+            ns_cluster_sync();
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t at = as + (uint32_t)(row * 512 + ((16 * half + 8 * part + j) ^ (row & 31)) * 16);
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (uint32_t c = 0; c < ctas; ++c) {
+                        const float4 v = ns_read_peer(at, c);
+                        sum.x += v.x;
+                        sum.y += v.y;
+                        sum.z += v.z;
+                        sum.w += v.w;
+                    }
+                    av[part][4 * j] = sum.x;
+                    av[part][4 * j + 1] = sum.y;
+                    av[part][4 * j + 2] = sum.z;
+                    av[part][4 * j + 3] = sum.w;
+                }
+            ns_cluster_sync();
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) write32(as_p, 64 * half + 32 * part, av[part]);
+        publish();
+        // A A, then P = a I + b A + c A A over it
+        if (warp == 0 && ok) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint64_t h = tc_desc_k(as + b * kBlockBytes), l = tc_desc_k(as + b * kBlockBytes + kHalfBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) {
+                    tc_mma(tmem, l + 2 * j, h + 2 * j, square, b != 0 || j != 0);
+                    tc_mma(tmem, h + 2 * j, l + 2 * j, square, 1u);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint64_t h = tc_desc_k(as + b * kBlockBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(tmem + 128 * b, h + 2 * j, h + 2 * j, square, b == 0 || j != 0);
+            }
+        }
+        finish();
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const int col = 64 * half + 32 * part;
+            float o[32];
+            read32(col, 2, 128, o);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                o[j] = fmaf(a.s.p_a[step], av[part][j], a.s.p[step] * o[j]);
+                if (col + j == row) o[j] += a.s.p_diag[step];
+            }
+            write32(as_p, col, o);
+        }
+        publish();
+        // P X: K is r here, a row of X a row along K
+        if (warp == 0 && ok) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint64_t h = tc_desc_k(as + b * kBlockBytes), l = tc_desc_k(as + b * kBlockBytes + kHalfBytes);
+                const uint64_t xh = tc_desc_mn(xs + b * 64 * 128, kBlockBytes), xl = tc_desc_mn(xs + kHalfBytes + b * 64 * 128, kBlockBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) {
+                    tc_mma(tmem, l + 2 * j, xh + (2048 >> 4) * j, wide, b != 0 || j != 0);
+                    tc_mma(tmem, h + 2 * j, xl + (2048 >> 4) * j, wide, 1u);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint64_t h = tc_desc_k(as + b * kBlockBytes), xh = tc_desc_mn(xs + b * 64 * 128, kBlockBytes);
+#pragma unroll
+                for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(tmem + 256 * b, h + 2 * j, xh + (2048 >> 4) * j, wide, b == 0 || j != 0);
+            }
+        }
+        finish();
+        const bool last = step + 1 == a.steps;
+        for (int col = 32 * half; col < a.cols; col += 64) {
+            float o[32];
+            read32(col, 2, 256, o);
+            if (!last) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] *= a.s.apply[step];
+                write32(base_p, col, o);
+                continue;
+            }
+            if (!ok) continue;
+            auto store = [&](int64_t i, int64_t j, float v) {
+                const int64_t at = batch * a.out_batch + i * a.ldo + j;
+                if (src.dtype == GNNPRE_F32) static_cast<float*>(a.out)[at] = v;
+                else if (src.dtype == GNNPRE_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+                else static_cast<__half*>(a.out)[at] = __float2half_rn(v);
+            };
+            if (src.tall) {  // neighbouring lanes are neighbours in out's rows
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (row < r && j0 + col + j < n) store(j0 + col + j, row, o[j] * a.out_factor);
+            } else {
+                float* line = reinterpret_cast<float*>(as_p) + warp * (32 * 33);  // (P has been read)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) line[lane * 33 + j] = o[j] * a.out_factor;
+                __syncwarp();
+                if (j0 + col + lane < n)
+                    for (int i = 0; i < 32 && 32 * q + i < r; ++i) store(32 * q + i, j0 + col + lane, line[i * 33 + lane]);
+                __syncwarp();
+            }
+        }
+        tc_fence_before();
+    }
+    if (warp == 0) {
+        tc_commit(drained);
+        for (uint32_t i = 0; i < kTcSpinLimit; ++i)
+            if (tc_bar_test(drained, 0)) break;
+    }
+    if (ctas > 1) ns_cluster_sync();  // nobody reads this CTA's memory any more
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        tc_free(tmem, 512);
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ host
 
 struct Bounds {
@@ -482,6 +1150,8 @@ int exponent_for(double bound) { return std::max(-8, std::min(14, (int)std::floo
 struct NsShape {
     int64_t r, n, rp, np, batch;
     int32_t segment;  // steps at most between two X
+    int32_t ctas;     // of the cluster that does all of a matrix; 0: a launch per product
+    bool chip;        // ... from shared memory
     int64_t side, square;  // bytes of one split [rp, np], [rp, rp]
     int64_t xt[2], x, a, t, p, q[2], partial, total;
 };
@@ -498,7 +1168,14 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     s.np = (s.n + 127) / 128 * 128;
     // multiplications per step of a segment of g steps, in units of r^2: n + 2 n for its ends, (4 g - 3) r between
     const auto cost = [&](int g) { return (3.0 * s.np + (4.0 * g - 3.0) * s.rp) / g; };
+    // One cluster per matrix while a CTA of it has few tiles in a product.
+    const int64_t tiles = s.rp / 128 * (s.np / kClusterTile);
+    s.ctas = tiles > kMostClusterTiles ? 0 : tiles > 8 && batch <= 6 ? 16 : 8;
+    s.chip = s.r <= 128 && s.n <= kChipCols * kChipMaxCtas;
+    if (s.chip)
+        for (s.ctas = 1; s.ctas * kChipCols < s.n;) s.ctas *= 2;
     s.segment = 1;
+    if (s.ctas) most = 1;
     for (int g = 2; g <= std::min(most, steps); ++g)
         if (cost(g) < 0.99 * cost(s.segment)) s.segment = g;
     s.side = s.rp * s.np * 4;
@@ -509,9 +1186,14 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
         at += (bytes * batch + 1023) / 1024 * 1024;
         return here;
     };
+    if (s.chip) {
+        s.partial = take((int64_t)sizeof(double) * kNormBlocks);
+        s.total = at;
+        return s;
+    }
     s.x = take(s.side);
     s.xt[0] = take(s.side);
-    s.xt[1] = steps > s.segment ? take(s.side) : s.xt[0];
+    s.xt[1] = steps > s.segment || s.ctas ? take(s.side) : s.xt[0];
     s.a = take(s.square);
     s.p = take(s.square);
     s.q[0] = s.segment > 1 ? take(s.square) : s.p;
@@ -526,6 +1208,32 @@ struct NsSelfTest {
     int32_t drop;
     uint32_t polls;
 };
+
+// One cluster of `ctas` CTAs per matrix.
+template <typename Args>
+int launch_clusters(void (*kernel)(Args), unsigned threads, int smem, int32_t ctas, int64_t batch, cudaStream_t st, const Args& args) {
+    static std::atomic<bool> opted_in[kMaxDevices];  // (per kernel: their arguments' types differ)
+    int dev = 0;
+    GNNPRE_CUDA(cudaGetDevice(&dev));
+    if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
+        GNNPRE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        GNNPRE_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
+    }
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(batch * ctas));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    GNNPRE_CUDA(cudaLaunchKernelEx(&cfg, kernel, args));
+    return GNNPRE_OK;
+}
 
 template <int BN>
 int launch_product_n(const Product& a, int64_t tiles_m, int64_t batch, cudaStream_t st) {
@@ -580,6 +1288,46 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
     int ex = exponent_for(bound.x[0]);
     Source src{G, ldg, g_stride, (int32_t)rows, (int32_t)cols, dtype, rows > cols, (double)eps, reinterpret_cast<double*>(w + s.partial),
                (float)std::ldexp(1.0, ex), side(s.x), side_t(s.xt[0])};
+    Steps factors{};
+    float out_factor = 0.f;
+    if (s.ctas)
+        for (int32_t k = 0; k < steps; ++k) {
+            const int ea = exponent_for(bound.x[k] * bound.x[k]), ep = exponent_for(bound.p[k]), ex_new = exponent_for(bound.x[k + 1]);
+            factors.gram[k] = (float)std::ldexp(1.0, ea - 2 * ex);
+            factors.p[k] = (float)std::ldexp((double)coeffs[2], ep - 2 * ea);
+            factors.p_a[k] = (float)std::ldexp((double)coeffs[1], ep - ea);
+            factors.p_diag[k] = (float)std::ldexp((double)coeffs[0], ep);
+            factors.apply[k] = (float)std::ldexp(1.0, ex_new - ep - ex);
+            out_factor = (float)std::ldexp((double)scale, -ep - ex);  // of the last step
+            ex = ex_new;
+        }
+    if (s.chip) {
+        const int64_t cols = ((s.n + s.ctas - 1) / s.ctas + 63) / 64 * 64;
+        const Chip c{src, (int32_t)cols, steps, out, ldo, o_stride, out_factor, error_flag, test ? test->polls : kTcSpinLimit, test ? test->drop : 0, factors};
+        return launch_clusters(k_ns_chip, kChipThreads, kChipSmem, s.ctas, batch, st, c);
+    }
+    if (s.ctas) {
+        Cluster c{};
+        c.src = src;
+        c.a = square(s.a);
+        c.p = square(s.p);
+        c.xt[0] = side_t(s.xt[0]);
+        c.xt[1] = side_t(s.xt[1]);
+        c.rp = (int32_t)s.rp;
+        c.np = (int32_t)s.np;
+        c.k_r = (int32_t)((s.r + 63) / 64);
+        c.k_n = (int32_t)((s.n + 63) / 64);
+        c.steps = steps;
+        c.out = out;
+        c.ldo = ldo;
+        c.out_batch = o_stride;
+        c.error = error_flag;
+        c.spin_limit = test ? test->polls : kTcSpinLimit;
+        c.drop = test ? test->drop : 0;
+        c.out_factor = out_factor;
+        c.s = factors;
+        return launch_clusters(k_ns_cluster, kProductThreads, kClusterSmem, s.ctas, batch, st, c);
+    }
     const int norm_blocks = (int)std::min<int64_t>(kNormBlocks, rows);
     k_ns_norm<<<dim3((unsigned)norm_blocks, (unsigned)batch), kNormThreads, 0, st>>>(src);
     GNNPRE_CUDA(cudaGetLastError());
