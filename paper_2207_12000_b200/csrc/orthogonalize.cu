@@ -58,7 +58,9 @@ __device__ __forceinline__ uint32_t block_byte(int row, int col) {
     return (uint32_t)(row * 128 + ((((col >> 3) ^ (row & 7)) & 7) << 4) + (col & 7) * 2);
 }
 
-// v as 2^e v in two fp16 numbers, eight of them at a time.
+// v in two fp16 numbers, eight of them at a time.  The high part is rounded to nearest: cut from v's upper bits (two conversions less,
+// no faster here) it leaves a low part of v's sign, whose squares, which are not computed, then add up in A's diagonal: 3.1e-6 off
+// on [256, 128] for 1.9e-6.
 __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
     uint32_t h[4], l[4];
 #pragma unroll
@@ -159,12 +161,13 @@ __global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t 
 
 // ------------------------------------------------------------------------------------------------ products
 
-// D = alpha * (A B^T) + beta * C + diag * I over the stored (scaled) numbers.
+// D = alpha * (A B^T) + diag * I over the stored (scaled) numbers.  Where D is a new A, its second form c A + b I is written too:
+// P = a I + A (c A + b I) then needs no A beside its accumulator (read from memory there it took 4.5 us of a product's 7.5).
 struct Job {
-    Split a, b, c, d, dt;
-    float alpha, beta, diag;
+    Split a, b, d, dt, d2;
+    float alpha, diag, alpha2, diag2;
     int32_t k_chunks;
-    int32_t has_c, write_t;  // write_t: D's transpose as well
+    int32_t write_t, write_2;  // write_t: D's transpose as well
 };
 
 struct Product {
@@ -362,69 +365,61 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
         // those is a column of the tile); both go out as they lie.
         const bool transposed = job.write_t || (a.symmetric && bi != bj);
         unsigned char* const tile_t = base_p + BN / kBlockCols * kBlockBytes;
-        if (warp < kSumWarps)
+        for (int form = 0; form < 1 + job.write_2; ++form) {
+            const Split& to = form ? job.d2 : job.d;
+            const float alpha = form ? job.alpha2 : job.alpha, on_diag = form ? job.diag2 : job.diag;
+            if (form) __syncthreads();  // (the first form's copies have read their tiles: thread 0 has waited)
+            if (warp < kSumWarps)
 #pragma unroll
-            for (int part = 0; part < kCols / 32; ++part) {
-                const int c0 = half * kCols + 32 * part;
-                const int col0 = bj * BN + c0;  // of D
-                const int diag = bi * kBlockRows + row - col0;  // the column of these 32 that lies on the diagonal
-                const unsigned char* c = job.has_c ? job.c.block(batch, bi, col0 / kBlockCols) : nullptr;
+                for (int part = 0; part < kCols / 32; ++part) {
+                    const int c0 = half * kCols + 32 * part;
+                    const int diag = bi * kBlockRows + row - (bj * BN + c0);  // the column of these 32 that lies on the diagonal
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float o[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = job.alpha * sum[32 * part + 8 * j + e];
-                    if (job.has_c) {
-                        const uint4 ch = *reinterpret_cast<const uint4*>(c + block_byte(row, col0 % kBlockCols + 8 * j));
-                        const uint4 cl = *reinterpret_cast<const uint4*>(c + kHalfBytes + block_byte(row, col0 % kBlockCols + 8 * j));
-                        const __half2* h = reinterpret_cast<const __half2*>(&ch);
-                        const __half2* l = reinterpret_cast<const __half2*>(&cl);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 fh = __half22float2(h[e]), fl = __half22float2(l[e]);
-                            o[2 * e] = fmaf(job.beta, fh.x + fl.x, o[2 * e]);
-                            o[2 * e + 1] = fmaf(job.beta, fh.y + fl.y, o[2 * e + 1]);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (8 * j + e == diag) o[e] += job.diag;
-                    uint4 hi, lo;
-                    split8(o, hi, lo);
-                    unsigned char* d = base_p + c0 / kBlockCols * kBlockBytes + block_byte(row, c0 % kBlockCols + 8 * j);
-                    *reinterpret_cast<uint4*>(d) = hi;
-                    *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
-                    if (transposed) {
-                        const __half* h = reinterpret_cast<const __half*>(&hi);
-                        const __half* l = reinterpret_cast<const __half*>(&lo);
+                    for (int j = 0; j < 4; ++j) {
+                        float o[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            unsigned char* t = tile_t + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
-                            *reinterpret_cast<__half*>(t) = h[e];
-                            *reinterpret_cast<__half*>(t + kBBytes) = l[e];
+                            o[e] = alpha * sum[32 * part + 8 * j + e];
+                            if (8 * j + e == diag) o[e] += on_diag;
+                        }
+                        uint4 hi, lo;
+                        split8(o, hi, lo);
+                        unsigned char* d = base_p + c0 / kBlockCols * kBlockBytes + block_byte(row, c0 % kBlockCols + 8 * j);
+                        *reinterpret_cast<uint4*>(d) = hi;
+                        *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+                        if (transposed) {
+                            const __half* h = reinterpret_cast<const __half*>(&hi);
+                            const __half* l = reinterpret_cast<const __half*>(&lo);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                unsigned char* t = tile_t + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
+                                *reinterpret_cast<__half*>(t) = h[e];
+                                *reinterpret_cast<__half*>(t + kBBytes) = l[e];
+                            }
                         }
                     }
                 }
-            }
-        tc_fence_async();
-        __syncthreads();
-        if (threadIdx.x == 0) {
+            tc_fence_async();
+            __syncthreads();
+            if (threadIdx.x == 0) {
 #pragma unroll
-            for (int b = 0; b < BN / kBlockCols; ++b)
-                tc_bulk_store(job.d.block(batch, bi, bj * (BN / kBlockCols) + b), base + b * kBlockBytes, kBlockBytes);
-            if (transposed) {
-                const Split& to = job.write_t ? job.dt : job.d;
-                const int rows0 = bj * BN % kBlockRows;
-                const uint32_t from = base + BN / kBlockCols * kBlockBytes;
+                for (int b = 0; b < BN / kBlockCols; ++b)
+                    tc_bulk_store(to.block(batch, bi, bj * (BN / kBlockCols) + b), base + b * kBlockBytes, kBlockBytes);
+                if (transposed) {
+                    const Split& to_t = job.write_t ? job.dt : to;
+                    const int rows0 = bj * BN % kBlockRows;
+                    const uint32_t from = base + BN / kBlockCols * kBlockBytes;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    unsigned char* t = to.block(batch, bj * BN / kBlockRows, 2 * bi + b) + rows0 * 128;
-                    tc_bulk_store(t, from + b * 2 * kBBytes, kBBytes);
-                    tc_bulk_store(t + kHalfBytes, from + b * 2 * kBBytes + kBBytes, kBBytes);
+                    for (int b = 0; b < 2; ++b) {
+                        unsigned char* t = to_t.block(batch, bj * BN / kBlockRows, 2 * bi + b) + rows0 * 128;
+                        tc_bulk_store(t, from + b * 2 * kBBytes, kBBytes);
+                        tc_bulk_store(t + kHalfBytes, from + b * 2 * kBBytes + kBBytes, kBBytes);
+                    }
                 }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                if (form < job.write_2) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             }
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     }
     if (warp == kMmaWarp) {
@@ -439,14 +434,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
 // for one another between products (three per step).  A product by itself takes some 7.5 us as a launch of its own: its CTAs
 // start, set up barriers and tensor memory, wait for the first copies, and leave.
 struct Steps {
-    float gram[kMaxSteps];                                   // alpha of A = X X^T
-    float p[kMaxSteps], p_a[kMaxSteps], p_diag[kMaxSteps];   // alpha, beta and diag of P
-    float apply[kMaxSteps];                                  // alpha of X = P X
+    float gram[kMaxSteps];                        // alpha of A = X X^T
+    float gram2[kMaxSteps], diag2[kMaxSteps];     // alpha and diag of its second form (one launch: of c A A and b A in P)
+    float p[kMaxSteps], p_diag[kMaxSteps];        // alpha and diag of P
+    float apply[kMaxSteps];                       // alpha of X = P X
 };
 
 struct Cluster {
     Source src;
-    Split a, p, xt[2];   // (x and xt[0] are the source's)
+    Split a, a2, p, xt[2];   // (x and xt[0] are the source's)
     int32_t rp, np, k_r, k_n, steps;
     void* out;
     int64_t ldo, out_batch;
@@ -584,7 +580,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
         const bool last = stage == 3 * a.steps - 1, tall = last && src.tall;
         const Split& xt = a.xt[step & 1];
         const Split& sa = kind == 0 ? src.x : kind == 1 ? a.a : tall ? xt : a.p;
-        const Split& sb = kind == 0 ? src.x : kind == 1 ? a.a : tall ? a.p : xt;
+        const Split& sb = kind == 0 ? src.x : kind == 1 ? a.a2 : tall ? a.p : xt;
         const int rows = tall ? a.np : a.rp, cols = kind < 2 || tall ? a.rp : a.np;
         const int k_chunks = kind == 0 ? a.k_n : a.k_r, tiles_n = cols / BN, all = rows / kBlockRows * tiles_n;
         for (int t = rank; t < all; t += ctas) {
@@ -627,60 +623,49 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
                     __syncwarp();
                     continue;
                 }
-                const float alpha = kind == 0 ? a.s.gram[step] : kind == 1 ? a.s.p[step] : a.s.apply[step];
-                const float beta = a.s.p_a[step], on_diag = a.s.p_diag[step];
-                const int c0 = half * kCols, col0 = bj * BN + c0, diag = bi * kBlockRows + row - col0;
-                uint4 ch[4], cl[4];
-                if (kind == 1) {
-                    const unsigned char* c = a.a.block(batch, bi, col0 / kBlockCols);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        ch[j] = __ldcg(reinterpret_cast<const uint4*>(c + block_byte(row, col0 % kBlockCols + 8 * j)));
-                        cl[j] = __ldcg(reinterpret_cast<const uint4*>(c + kHalfBytes + block_byte(row, col0 % kBlockCols + 8 * j)));
-                    }
-                }
+                const int c0 = half * kCols, diag = bi * kBlockRows + row - (bj * BN + c0);
                 // the staging is free when the last tile's copies have read it
                 if (threadIdx.x == 0 && stored) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 ns_sum_warps_sync();
+                auto stage_tile = [&](unsigned char* to, float alpha, float on_diag, bool transpose) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float o[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = alpha * sum[8 * j + e];
-                    if (kind == 1) {
-                        const __half2* h = reinterpret_cast<const __half2*>(&ch[j]);
-                        const __half2* l = reinterpret_cast<const __half2*>(&cl[j]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 fh = __half22float2(h[e]), fl = __half22float2(l[e]);
-                            o[2 * e] = fmaf(beta, fh.x + fl.x, o[2 * e]);
-                            o[2 * e + 1] = fmaf(beta, fh.y + fl.y, o[2 * e + 1]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (8 * j + e == diag) o[e] += on_diag;
-                    }
-                    uint4 hi, lo;
-                    split8(o, hi, lo);
-                    unsigned char* d = staging_p + block_byte(row, c0 + 8 * j);
-                    *reinterpret_cast<uint4*>(d) = hi;
-                    *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
-                    if (kind == 2) {
-                        const __half* h = reinterpret_cast<const __half*>(&hi);
-                        const __half* l = reinterpret_cast<const __half*>(&lo);
+                    for (int j = 0; j < 4; ++j) {
+                        float o[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            unsigned char* u = staging_p + kBlockBytes + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
-                            *reinterpret_cast<__half*>(u) = h[e];
-                            *reinterpret_cast<__half*>(u + kBBytes) = l[e];
+                            o[e] = alpha * sum[8 * j + e];
+                            if (8 * j + e == diag) o[e] += on_diag;
+                        }
+                        uint4 hi, lo;
+                        split8(o, hi, lo);
+                        unsigned char* d = to + block_byte(row, c0 + 8 * j);
+                        *reinterpret_cast<uint4*>(d) = hi;
+                        *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+                        if (transpose) {
+                            const __half* h = reinterpret_cast<const __half*>(&hi);
+                            const __half* l = reinterpret_cast<const __half*>(&lo);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                unsigned char* u = staging_p + kBlockBytes + row / kBlockCols * (2 * kBBytes) + block_byte(c0 + 8 * j + e, row % kBlockCols);
+                                *reinterpret_cast<__half*>(u) = h[e];
+                                *reinterpret_cast<__half*>(u + kBBytes) = l[e];
+                            }
                         }
                     }
+                };
+                if (kind == 0) {
+                    stage_tile(staging_p, a.s.gram[step], 0.f, false);
+                    stage_tile(staging_p + kBlockBytes, a.s.gram2[step], a.s.diag2[step], false);
+                } else if (kind == 1) {
+                    stage_tile(staging_p, a.s.p[step], a.s.p_diag[step], false);
+                } else {
+                    stage_tile(staging_p, a.s.apply[step], 0.f, true);
                 }
                 tc_fence_async();
                 ns_sum_warps_sync();
                 if (threadIdx.x == 0) {
-                    const Split& to = kind == 0 ? a.a : kind == 1 ? a.p : src.x;
-                    tc_bulk_store(to.block(batch, bi, bj), staging, kBlockBytes);
+                    tc_bulk_store((kind == 0 ? a.a : kind == 1 ? a.p : src.x).block(batch, bi, bj), staging, kBlockBytes);
+                    if (kind == 0) tc_bulk_store(a.a2.block(batch, bi, bj), staging + kBlockBytes, kBlockBytes);
                     if (kind == 2) {
                         const int rows0 = bj * BN % kBlockRows;
 #pragma unroll
@@ -769,13 +754,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
 // With r <= 128 all r x r matrices are one tile, and X (or, of a long one, a CTA's share of its columns) stays in shared memory
 // from the first step to the last.  It serves A = X X^T as both operands, rows along K, and P X as operand B as it lies: a row
 // of X is a row along K there (MN-major).  The CTAs of a cluster add up their shares' A, in the order of their ranks, and each
-// computes P for itself.  The eight warps read the accumulators: warps w and w + 4 share lanes 32 (w & 3) .., a half of the
-// columns each; A stays in their registers for P.  As each K-chunk's large terms have an accumulator of their own, four cuts of the
-// tensor core meet in a sum.
-constexpr int kChipThreads = 256;
+// computes P for itself.  The sixteen warps read the accumulators: warps w, w + 4, w + 8 and w + 12 share lanes 32 (w & 3) .., and take
+// 32-column pieces in turn; A stays in their registers for P.  (With eight warps reading, splitting and storing took 13,000 of a
+// step's 21,000 cycles on [256, 128], with the products, 96 of them, at the tensor core's rate in the rest.)  As each K-chunk's
+// large terms have an accumulator of their own, four cuts of the tensor core meet in a sum.
+constexpr int kChipThreads = 512;
 constexpr int kChipCols = 256;                       // columns of X in a CTA
 constexpr int kChipMaxCtas = 8;
-constexpr int kChipSmem = (kChipCols / kBlockCols + 2) * kBlockBytes + 1024;
+constexpr int kChipSmem = (kChipCols / kBlockCols + 3) * kBlockBytes + 1024;  // X, A or P, and room for half of a sum over the CTAs
 
 struct Chip {
     Source src;          // (x, xt: unused)
@@ -808,6 +794,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
     __shared__ double room[kChipThreads / 32], norm;
+    __shared__ float largest[kChipThreads / 32];
     volatile int* abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank, ctas;
@@ -833,42 +820,77 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
     const Source& src = a.src;
     const int r = src.tall ? src.cols : src.rows, n = src.tall ? src.rows : src.cols;
     const int j0 = (int)rank * a.cols, blocks = a.cols / kBlockCols;
-    const int q = warp & 3, half = warp >> 2, row = 32 * q + lane;
+    const int q = warp & 3, piece = warp >> 2, row = 32 * q + lane;  // this thread's lane of the accumulators, its piece of 128 columns
 
-    // This thread's row of X, a half of the share's columns: groups of eight, all read before the norm is known.
     {
-        constexpr int kGroups = kChipCols / 16;
-        float g[kGroups][8];
-        double sum2 = 0;
-        // (no load depends on a condition, so that all are under way together: what does not exist is read at the matrix's edge)
+        // G is read along its rows and laid down as fp32 where X will be: rows of 64 16-byte pieces, turned by the row.  Then every thread
+        // takes 64 columns of a row of X, and once all have theirs, X in two parts takes the place.
+        constexpr int kWarps = kChipThreads / 32;
+        auto place = [&](int i, int j) { return base_p + i * (kChipCols * 4) + (((j >> 2) ^ (i & 31)) << 4) + (j & 3) * 4; };
         auto load = [&](auto* p) {
-            p += batch * src.batch_stride + (int64_t)min(row, r - 1) * (src.tall ? 1 : src.ldg);
-            const int64_t apart = src.tall ? src.ldg : 1;
+            p += batch * src.batch_stride;
+            if (src.tall) {  // a row of G is a column of X: lanes are rows of X
+#pragma unroll 4
+                for (int j = warp; j < a.cols; j += kWarps)
 #pragma unroll
-            for (int k = 0; k < kGroups; ++k)
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = 32 * k + lane;
+                        const float v = to_f32(p[(int64_t)min(j0 + j, n - 1) * src.ldg + min(i, r - 1)]);
+                        *reinterpret_cast<float*>(place(i, j)) = i < r && j0 + j < n ? v : 0.f;
+                    }
+            } else {
+#pragma unroll 2
+                for (int i = warp; i < 128; i += kWarps)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[k][e] = to_f32(p[min(j0 + 8 * (2 * k + half) + e, n - 1) * apart]);
+                    for (int k = 0; k < kChipCols / 32; ++k) {
+                        const int j = 32 * k + lane;
+                        const float v = to_f32(p[(int64_t)min(i, r - 1) * src.ldg + min(j0 + j, n - 1)]);
+                        *reinterpret_cast<float*>(place(i, j)) = i < r && j < a.cols && j0 + j < n ? v : 0.f;
+                    }
+            }
         };
         if (src.dtype == GNNPRE_F32) load(static_cast<const float*>(src.g));
         else if (src.dtype == GNNPRE_BF16) load(static_cast<const __nv_bfloat16*>(src.g));
         else load(static_cast<const __half*>(src.g));
+        __syncthreads();
+        constexpr int kGroups = kChipCols / 32;  // of eight columns
+        float g[kGroups][8], most = 0.f;
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            const int c = 8 * (4 * k + piece);
+            if (c >= a.cols) continue;
+            const float4 u = *reinterpret_cast<const float4*>(place(row, c)), w = *reinterpret_cast<const float4*>(place(row, c + 4));
+            g[k][0] = u.x, g[k][1] = u.y, g[k][2] = u.z, g[k][3] = u.w;
+            g[k][4] = w.x, g[k][5] = w.y, g[k][6] = w.z, g[k][7] = w.w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(g[k][e]));
+        }
+        // squares of numbers of size one: neither tiny nor huge updates lose their norm
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if (lane == 0) largest[warp] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) most = fmaxf(most, largest[w]);
+        const int exponent = most > 0.f && most <= 3.4e38f ? min(max(ilogbf(most), -126), 126) : 0;
+        const float to_one = ldexpf(1.f, -exponent);
+        float sumf = 0.f;
 #pragma unroll
         for (int k = 0; k < kGroups; ++k)
+            if (8 * (4 * k + piece) < a.cols)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = 8 * (2 * k + half) + e;
-                if (c >= a.cols || row >= r || j0 + c >= n) g[k][e] = 0.f;
-            }
-#pragma unroll
-        for (int k = 0; k < kGroups; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum2 += (double)g[k][e] * g[k][e];
+                for (int e = 0; e < 8; ++e) {
+                    g[k][e] *= to_one;
+                    sumf = fmaf(g[k][e], g[k][e], sumf);
+                }
+        double sum2 = (double)sumf;
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) sum2 += __shfl_xor_sync(0xffffffffu, sum2, d);
         if (lane == 0) room[warp] = sum2;
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < kChipThreads / 32; ++w) sum2 += room[w];
+            for (int w = 1; w < kWarps; ++w) sum2 += room[w];
+            sum2 = ldexp(sum2, 2 * exponent);
             if (ctas > 1) src.partial[batch * kNormBlocks + rank] = sum2;
             else norm = sum2;
         }
@@ -881,15 +903,15 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             }
         }
         __syncthreads();
-        const double scale = 1.0 / (sqrt(norm) + src.eps) * (double)src.factor;
+        const float scale = (float)ldexp(1.0 / (sqrt(norm) + src.eps) * (double)src.factor, exponent);
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
-            const int c = 8 * (2 * k + half);
+            const int c = 8 * (4 * k + piece);
             if (c >= a.cols) continue;
             float v[8];
             uint4 hi, lo;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)((double)g[k][e] * scale);
+            for (int e = 0; e < 8; ++e) v[e] = g[k][e] * scale;
             split8(v, hi, lo);
             unsigned char* d = base_p + c / kBlockCols * kBlockBytes + block_byte(row, c % kBlockCols);
             *reinterpret_cast<uint4*>(d) = hi;
@@ -917,13 +939,27 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
     // sums of `accs` accumulators `apart` columns apart, 32 columns from `col`
     auto read32 = [&](int col, int accs, int apart, float (&sum)[32]) {
         uint32_t v[32];
+        tc_load32(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)col, v);
+        tc_load_wait();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) sum[j] = 0.f;
-        for (int k = 0; k < accs; ++k) {
+        for (int j = 0; j < 32; ++j) sum[j] = __uint_as_float(v[j]);
+        for (int k = 1; k < accs; ++k) {
             tc_load32(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(k * apart + col), v);
             tc_load_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) sum[j] += __uint_as_float(v[j]);
+            for (int j = 0; j < 32; j += 2) {
+                const float2 two = __fadd2_rn(make_float2(sum[j], sum[j + 1]), make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
+                sum[j] = two.x;
+                sum[j + 1] = two.y;
+            }
+        }
+    };
+    auto times = [&](float (&o)[32], float f) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float2 two = __fmul2_rn(make_float2(o[j], o[j + 1]), make_float2(f, f));
+            o[j] = two.x;
+            o[j + 1] = two.y;
         }
     };
     // 32 of this thread's numbers to columns col.. of the blocks at p
@@ -960,47 +996,47 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             }
         }
         finish();
-        float av[2][32];
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int col = 64 * half + 32 * part;
-            read32(col, blocks, 128, av[part]);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) av[part][j] *= a.s.gram[step];
-        }
+        float av[32];
+        read32(32 * piece, blocks, 128, av);
+        times(av, a.s.gram[step]);
         if (ctas > 1) {
-            // the shares' sums, laid down where A will be: rows of 32 pieces of 16 bytes, turned by the row
+            // The shares' sums, laid down where A will be: rows of 32 pieces of 16 bytes, turned by the row.  Half of the rows at a time
+            // the CTAs' are read piece by piece as they lie, neighbouring lanes neighbouring pieces (a lane to a row: 40 us a step
+            // with four CTAs), and added up in a place of their own.
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int piece = (16 * half + 8 * part + j) ^ (row & 31);
-                    *reinterpret_cast<float4*>(as_p + row * 512 + piece * 16) =
-                        make_float4(av[part][4 * j], av[part][4 * j + 1], av[part][4 * j + 2], av[part][4 * j + 3]);
-                }
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<float4*>(as_p + row * 512 + ((8 * piece + j) ^ (row & 31)) * 16) =
+                    make_float4(av[4 * j], av[4 * j + 1], av[4 * j + 2], av[4 * j + 3]);
             ns_cluster_sync();
+            unsigned char* const sum_p = as_p + 2 * kBlockBytes;
+            for (int part = 0; part < 2; ++part) {
+                constexpr int kPieces = kBlockBytes / 16 / kChipThreads;  // of a thread
+                float4 sum[kPieces];
+                for (uint32_t c = 0; c < ctas; ++c) {
+                    float4 v[kPieces];
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+                    for (int j = 0; j < kPieces; ++j) v[j] = ns_read_peer(as + (uint32_t)(part * kBlockBytes + (j * kChipThreads + (int)threadIdx.x) * 16), c);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t at = as + (uint32_t)(row * 512 + ((16 * half + 8 * part + j) ^ (row & 31)) * 16);
-                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (uint32_t c = 0; c < ctas; ++c) {
-                        const float4 v = ns_read_peer(at, c);
-                        sum.x += v.x;
-                        sum.y += v.y;
-                        sum.z += v.z;
-                        sum.w += v.w;
-                    }
-                    av[part][4 * j] = sum.x;
-                    av[part][4 * j + 1] = sum.y;
-                    av[part][4 * j + 2] = sum.z;
-                    av[part][4 * j + 3] = sum.w;
+                    for (int j = 0; j < kPieces; ++j)
+                        sum[j] = c == 0 ? v[j] : make_float4(sum[j].x + v[j].x, sum[j].y + v[j].y, sum[j].z + v[j].z, sum[j].w + v[j].w);
                 }
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) *reinterpret_cast<float4*>(sum_p + (j * kChipThreads + threadIdx.x) * 16) = sum[j];
+                __syncthreads();
+                if (row / 64 == part)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float4 v = *reinterpret_cast<const float4*>(sum_p + row % 64 * 512 + ((8 * piece + j) ^ (row & 31)) * 16);
+                        av[4 * j] = v.x;
+                        av[4 * j + 1] = v.y;
+                        av[4 * j + 2] = v.z;
+                        av[4 * j + 3] = v.w;
+                    }
+                __syncthreads();
+            }
             ns_cluster_sync();
         }
-#pragma unroll
-        for (int part = 0; part < 2; ++part) write32(as_p, 64 * half + 32 * part, av[part]);
+        write32(as_p, 32 * piece, av);
         publish();
         // A A, then P = a I + b A + c A A over it
         if (warp == 0 && ok) {
@@ -1021,15 +1057,22 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             }
         }
         finish();
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int col = 64 * half + 32 * part;
+        {
+            const int col = 32 * piece;
             float o[32];
             read32(col, 2, 128, o);
+            times(o, a.s.gram2[step]);
+            const float2 b = make_float2(a.s.diag2[step], a.s.diag2[step]);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                o[j] = fmaf(a.s.p_a[step], av[part][j], a.s.p[step] * o[j]);
-                if (col + j == row) o[j] += a.s.p_diag[step];
+            for (int j = 0; j < 32; j += 2) {
+                const float2 two = __ffma2_rn(b, make_float2(av[j], av[j + 1]), make_float2(o[j], o[j + 1]));
+                o[j] = two.x;
+                o[j + 1] = two.y;
+            }
+            if (piece == q) {  // the diagonal's warps
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j == lane) o[j] += a.s.p_diag[step];
             }
             write32(as_p, col, o);
         }
@@ -1055,12 +1098,11 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
         }
         finish();
         const bool last = step + 1 == a.steps;
-        for (int col = 32 * half; col < a.cols; col += 64) {
+        for (int col = 32 * piece; col < a.cols; col += 128) {
             float o[32];
             read32(col, 2, 256, o);
             if (!last) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] *= a.s.apply[step];
+                times(o, a.s.apply[step]);
                 write32(base_p, col, o);
                 continue;
             }
@@ -1076,12 +1118,12 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
                 for (int j = 0; j < 32; ++j)
                     if (row < r && j0 + col + j < n) store(j0 + col + j, row, o[j] * a.out_factor);
             } else {
-                float* line = reinterpret_cast<float*>(as_p) + warp * (32 * 33);  // (P has been read)
+                float* line = reinterpret_cast<float*>(as_p) + warp * (32 * 32);  // (P has been read); columns turned by the row
 #pragma unroll
-                for (int j = 0; j < 32; ++j) line[lane * 33 + j] = o[j] * a.out_factor;
+                for (int j = 0; j < 32; ++j) line[lane * 32 + (j ^ lane)] = o[j] * a.out_factor;
                 __syncwarp();
                 if (j0 + col + lane < n)
-                    for (int i = 0; i < 32 && 32 * q + i < r; ++i) store(32 * q + i, j0 + col + lane, line[i * 33 + lane]);
+                    for (int i = 0; i < 32 && 32 * q + i < r; ++i) store(32 * q + i, j0 + col + lane, line[i * 32 + (lane ^ i)]);
                 __syncwarp();
             }
         }
@@ -1147,13 +1189,16 @@ bool bounds_of(const float* coeffs, int32_t steps, Bounds* out) {
 // 2^e with which a matrix of this bound fits fp16 with room to spare.
 int exponent_for(double bound) { return std::max(-8, std::min(14, (int)std::floor(std::log2(32768.0 / std::max(bound, 1e-6))))); }
 
+// Of c A + b I, A's second form, where X has this bound.
+int second_exponent(const float* coeffs, double x) { return exponent_for(std::fabs(coeffs[2]) * x * x + std::fabs(coeffs[1])); }
+
 struct NsShape {
     int64_t r, n, rp, np, batch;
     int32_t segment;  // steps at most between two X
     int32_t ctas;     // of the cluster that does all of a matrix; 0: a launch per product
     bool chip;        // ... from shared memory
     int64_t side, square;  // bytes of one split [rp, np], [rp, rp]
-    int64_t xt[2], x, a, t, p, q[2], partial, total;
+    int64_t xt[2], x, a, a2, t, p, q[2], partial, total;
 };
 
 // Steps of a segment at most (see above).
@@ -1195,6 +1240,7 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     s.xt[0] = take(s.side);
     s.xt[1] = steps > s.segment || s.ctas ? take(s.side) : s.xt[0];
     s.a = take(s.square);
+    s.a2 = take(s.square);
     s.p = take(s.square);
     s.q[0] = s.segment > 1 ? take(s.square) : s.p;
     s.q[1] = s.segment > 1 ? take(s.square) : s.p;
@@ -1293,9 +1339,11 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
     if (s.ctas)
         for (int32_t k = 0; k < steps; ++k) {
             const int ea = exponent_for(bound.x[k] * bound.x[k]), ep = exponent_for(bound.p[k]), ex_new = exponent_for(bound.x[k + 1]);
+            const int e2 = s.chip ? ep : second_exponent(coeffs, bound.x[k]);
             factors.gram[k] = (float)std::ldexp(1.0, ea - 2 * ex);
-            factors.p[k] = (float)std::ldexp((double)coeffs[2], ep - 2 * ea);
-            factors.p_a[k] = (float)std::ldexp((double)coeffs[1], ep - ea);
+            factors.gram2[k] = (float)std::ldexp((double)coeffs[2], s.chip ? ep - 2 * ea : e2 - 2 * ex);
+            factors.diag2[k] = (float)std::ldexp((double)coeffs[1], s.chip ? ep - ea : e2);
+            factors.p[k] = (float)std::ldexp(1.0, ep - ea - e2);
             factors.p_diag[k] = (float)std::ldexp((double)coeffs[0], ep);
             factors.apply[k] = (float)std::ldexp(1.0, ex_new - ep - ex);
             out_factor = (float)std::ldexp((double)scale, -ep - ex);  // of the last step
@@ -1310,6 +1358,7 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
         Cluster c{};
         c.src = src;
         c.a = square(s.a);
+        c.a2 = square(s.a2);
         c.p = square(s.p);
         c.xt[0] = side_t(s.xt[0]);
         c.xt[1] = side_t(s.xt[1]);
@@ -1342,37 +1391,62 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
     int xt = 0;
     for (int32_t k = 0; k < steps;) {
         const int32_t g = std::min(s.segment, steps - k);
-        int ea = exponent_for(bound.x[k] * bound.x[k]);
+        int ea = exponent_for(bound.x[k] * bound.x[k]), e2 = second_exponent(coeffs, bound.x[k]);
+        // a new A from an accumulator that holds 2^acc of it
+        const auto new_a = [&](Job& job, int acc) {
+            job.d = square(s.a);
+            job.alpha = (float)std::ldexp(1.0, ea - acc);
+            job.d2 = square(s.a2);
+            job.alpha2 = (float)std::ldexp((double)coeffs[2], e2 - acc);
+            job.diag2 = (float)std::ldexp((double)coeffs[1], e2);
+            job.write_2 = 1;
+        };
+        const auto operands = [](const Split& x, const Split& y, int32_t chunks) {
+            Job job{};
+            job.a = x;
+            job.b = y;
+            job.k_chunks = chunks;
+            return job;
+        };
         Product m = base;
-        m.job[0] = Job{side(s.x), side(s.x), {}, square(s.a), {}, (float)std::ldexp(1.0, ea - 2 * ex), 0.f, 0.f, k_n, 0, 0};
+        m.job[0] = operands(side(s.x), side(s.x), k_n);
+        new_a(m.job[0], 2 * ex);
         GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
         int eq = 0, q = 0;
         double q_bound = 1;
         for (int32_t j = 0; j < g; ++j) {
-            // P = a I + b A + c A A
+            // P = a I + A (c A + b I)
             const int ep = exponent_for(bound.p[k + j]);
             const Split p = square(j == 0 ? s.q[0] : s.p);
             m = base;
-            m.job[0] = Job{square(s.a), square(s.a), square(s.a), p, {}, (float)std::ldexp((double)coeffs[2], ep - 2 * ea),
-                           (float)std::ldexp((double)coeffs[1], ep - ea), (float)std::ldexp((double)coeffs[0], ep), k_r, 1, 0};
+            m.job[0] = operands(square(s.a), square(s.a2), k_r);
+            m.job[0].d = p;
+            m.job[0].alpha = (float)std::ldexp(1.0, ep - ea - e2);
+            m.job[0].diag = (float)std::ldexp((double)coeffs[0], ep);
             GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
             q_bound *= bound.p[k + j];
             const int eq_new = j == 0 ? ep : exponent_for(q_bound);
-            const Job more = {square(s.q[q]), p, {}, square(s.q[q ^ 1]), {}, (float)std::ldexp(1.0, eq_new - eq - ep), 0.f, 0.f, k_r, 0, 0};
+            Job more = operands(square(s.q[q]), p, k_r);
+            more.d = square(s.q[q ^ 1]);
+            more.alpha = (float)std::ldexp(1.0, eq_new - eq - ep);
             m = base;
             if (j + 1 < g) {
                 // T = A P, then the next A = T P beside Q = Q P
-                const int et = exponent_for(bound.x[k + j] * bound.x[k + j] * bound.p[k + j]), ea_new = exponent_for(bound.x[k + j + 1] * bound.x[k + j + 1]);
-                m.job[0] = Job{square(s.a), p, {}, square(s.t), {}, (float)std::ldexp(1.0, et - ea - ep), 0.f, 0.f, k_r, 0, 0};
+                const int et = exponent_for(bound.x[k + j] * bound.x[k + j] * bound.p[k + j]);
+                m.job[0] = operands(square(s.a), p, k_r);
+                m.job[0].d = square(s.t);
+                m.job[0].alpha = (float)std::ldexp(1.0, et - ea - ep);
                 GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
+                ea = exponent_for(bound.x[k + j + 1] * bound.x[k + j + 1]);
+                e2 = second_exponent(coeffs, bound.x[k + j + 1]);
                 m = base;
-                m.job[0] = Job{square(s.t), p, {}, square(s.a), {}, (float)std::ldexp(1.0, ea_new - et - ep), 0.f, 0.f, k_r, 0, 0};
+                m.job[0] = operands(square(s.t), p, k_r);
+                new_a(m.job[0], et + ep);
                 if (j > 0) {
                     m.job[1] = more;
                     m.jobs = 2;
                 }
                 GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
-                ea = ea_new;
             } else if (j > 0) {
                 m.job[0] = more;
                 GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
@@ -1384,7 +1458,11 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
         m = base;
         if (k < steps) {
             const int ex_new = exponent_for(bound.x[k]);
-            m.job[0] = Job{square(s.q[q]), side_t(s.xt[xt]), {}, side(s.x), side_t(s.xt[xt ^ 1]), (float)std::ldexp(1.0, ex_new - eq - ex), 0.f, 0.f, k_r, 0, 1};
+            m.job[0] = operands(square(s.q[q]), side_t(s.xt[xt]), k_r);
+            m.job[0].d = side(s.x);
+            m.job[0].dt = side_t(s.xt[xt ^ 1]);
+            m.job[0].write_t = 1;
+            m.job[0].alpha = (float)std::ldexp(1.0, ex_new - eq - ex);
             GNNPRE_TRY(launch_product(m, s.rp, s.np, batch, false, sms, st));
             ex = ex_new;
             xt ^= 1;
@@ -1399,7 +1477,7 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
         m.out_factor = (float)std::ldexp((double)scale, -eq - ex);
         // Q is symmetric: the transpose of Q X is X^T Q
         const bool tall = rows > cols;
-        m.job[0] = Job{tall ? side_t(s.xt[xt]) : square(s.q[q]), tall ? square(s.q[q]) : side_t(s.xt[xt]), {}, {}, {}, 1.f, 0.f, 0.f, k_r, 0, 0};
+        m.job[0] = operands(tall ? side_t(s.xt[xt]) : square(s.q[q]), tall ? square(s.q[q]) : side_t(s.xt[xt]), k_r);
         GNNPRE_TRY(launch_product(m, tall ? s.np : s.rp, tall ? s.rp : s.np, batch, false, sms, st));
     }
     return GNNPRE_OK;

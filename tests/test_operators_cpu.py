@@ -96,7 +96,7 @@ def test_orthogonalize_workspace(lib):
     assert size(3, 256, 602, 5) == size(3, 602, 256, 5)  # the smaller side counts, not which it is
     for batch, rows, cols in ((1, 1, 1), (3, 256, 602), (1, 2048, 4096)):
         r, n = (-(-x // 128) * 128 for x in sorted((rows, cols)))
-        assert 0 < size(batch, rows, cols, 5) <= batch * (4 * (3 * r * n + 5 * r * r) + 512) + 16384
+        assert 0 < size(batch, rows, cols, 5) <= batch * (4 * (3 * r * n + 6 * r * r) + 512) + 16384
 
 
 def pointers(*p):
