@@ -65,7 +65,16 @@ struct LookupArgs {
     int32_t lanes;  // per row, a power of two
 };
 
-constexpr int kLookupThreads = 256;
+constexpr int kLookupThreads = 128;
+
+// Rows that this call does not read again: written past what the L2 keeps (2.4 M rows of 256 bf16 from a table that it holds: 508 us
+// without the hint, 373 with it, 357 in CTAs of 128 threads; the stores by themselves 330).
+template <typename T, int E>
+__device__ __forceinline__ void store_once(T* p, const Vec<T, E>& v) {
+    if constexpr (E * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
+    else if constexpr (E * sizeof(T) == 8) __stcs(reinterpret_cast<uint2*>(p), *reinterpret_cast<const uint2*>(&v));
+    else *reinterpret_cast<Vec<T, E>*>(p) = v;
+}
 
 // `lanes` threads per row and U rows per thread, whose reads are all in flight before the first is used.
 template <typename T, int E, int U>
@@ -94,7 +103,7 @@ __global__ void __launch_bounds__(kLookupThreads) k_lookup(const LookupArgs a) {
             if (!dst[u]) continue;
 #pragma unroll
             for (int e = 0; e < E; ++e) v[u].v[e] = src[u] ? from_f32<T>(to_f32(v[u].v[e]) * a.scale) : from_f32<T>(0.f);
-            *reinterpret_cast<Vec<T, E>*>(dst[u] + c) = v[u];
+            store_once(dst[u] + c, v[u]);
         }
     }
     for (int64_t c = whole + lane; c < a.dim; c += a.lanes)  // what does not fill an access
@@ -161,29 +170,34 @@ constexpr int kOneCtaThreads = 1024;
 constexpr int kOneCtaPerThread = 8;
 constexpr int kOneCtaKeys = kOneCtaThreads * kOneCtaPerThread;
 constexpr int kOneCtaDigit = 8;                  // bits
-constexpr int kSortThreads = 256;
-constexpr int kSortPerThread = 16;
+constexpr int kSortThreads = 512;
+constexpr int kSortPerThread = 8;
 constexpr int kSortKeys = kSortThreads * kSortPerThread;
 constexpr int kMaxDigit = 11;
 constexpr int kSelfScanBlocks = 32;              // up to here a block adds up the other blocks' counts itself
 
 // Places of one warp's keys among those with the same digit before them in this warp; `counts` is the warp's row of counters.
-// Rounds of 32 neighbouring keys, so the order is kept.
+// Rounds of 32 neighbouring keys, so the order is kept.  Lanes with the same digit are found bit by bit: the ballots of a round do
+// not wait for one another (match.any takes longer the more digits there are).
 template <int ROUNDS>
-__device__ __forceinline__ void rank_in_warp(const uint32_t (&digit)[ROUNDS], const bool (&live)[ROUNDS], uint16_t* counts,
-                                             uint32_t (&place)[ROUNDS]) {
+__device__ __forceinline__ void rank_in_warp(const uint32_t (&digit)[ROUNDS], const bool (&live)[ROUNDS], int bits, int rounds,
+                                             uint16_t* counts, uint32_t (&place)[ROUNDS]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
-        const uint32_t peers = __match_any_sync(0xffffffffu, live[r] ? digit[r] : 0xffffffffu);
-        const int leader = __ffs(peers) - 1;
-        uint32_t before = 0;
-        if (live[r] && lane == leader) {
-            before = counts[digit[r]];
-            counts[digit[r]] = (uint16_t)(before + __popc(peers));
+        if (r >= rounds) break;
+        uint32_t peers = __ballot_sync(0xffffffffu, live[r]);
+        for (int b = 0; b < bits; ++b) {
+            const bool bit = digit[r] >> b & 1u;
+            const uint32_t with = __ballot_sync(0xffffffffu, bit);
+            peers &= bit ? with : ~with;
         }
-        before = __shfl_sync(0xffffffffu, before, leader);
-        place[r] = before + __popc(peers & ((1u << lane) - 1u));
+        const uint32_t below = peers & ((1u << lane) - 1u);
+        uint32_t before = 0;
+        if (live[r]) before = counts[digit[r]];
+        __syncwarp();
+        if (live[r] && below == 0) counts[digit[r]] = (uint16_t)(before + __popc(peers));
+        place[r] = before + __popc(below);
         __syncwarp();
     }
 }
@@ -223,7 +237,7 @@ struct SortArgs {
     const uint32_t* pos_in;
     uint32_t* keys_out;
     uint32_t* pos_out;
-    uint32_t* counts;          // [digit][block]
+    uint32_t* counts;          // [digit][block] where they are scanned by a kernel of their own, else [block][digit]
     uint32_t* totals;          // [digit]
     Clear clear;
 };
@@ -238,12 +252,13 @@ __global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs 
     uint32_t* keys = reinterpret_cast<uint32_t*>(sort_smem);
     uint16_t* pos = reinterpret_cast<uint16_t*>(keys + kOneCtaKeys);
     uint16_t* counts = pos + kOneCtaKeys;  // [warp][digit]
+    __shared__ uint16_t firsts[4][1 << kOneCtaDigit];
     __shared__ uint32_t room[32];
     constexpr int kWarps = kOneCtaThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = (int)a.count;
     // neighbouring keys of a warp, in rounds that no thread needs more of than there are keys for
-    const int per_warp = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
+    const int per_warp = ((n + kWarps - 1) / kWarps + 31) / 32 * 32, rounds = per_warp / 32;
     const int passes = (key_bits + kOneCtaDigit - 1) / kOneCtaDigit, bits = (key_bits + passes - 1) / passes;
     uint32_t key[kOneCtaPerThread], place[kOneCtaPerThread], digit[kOneCtaPerThread];
     uint16_t at[kOneCtaPerThread];
@@ -251,35 +266,51 @@ __global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs 
 #pragma unroll
     for (int r = 0; r < kOneCtaPerThread; ++r) {
         const int i = warp * per_warp + 32 * r + lane;
-        live[r] = 32 * r < per_warp && i < n;
+        live[r] = r < rounds && i < n;
         at[r] = (uint16_t)i;
         key[r] = live[r] ? id_at(a.ids, i) : 0u;
     }
+    const int digits = 1 << bits;
     for (int p = 0; p < passes; ++p) {
-        const int shift = p * bits, digits = 1 << bits;
-        for (int i = threadIdx.x; i < kWarps * digits; i += kOneCtaThreads) counts[i] = 0;
+        const int shift = p * bits;
+        for (int i = threadIdx.x; i < kWarps * digits / 2; i += kOneCtaThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kOneCtaPerThread; ++r) digit[r] = (key[r] >> shift) & (uint32_t)(digits - 1);
-        rank_in_warp<kOneCtaPerThread>(digit, live, counts + warp * digits, place);
+        rank_in_warp<kOneCtaPerThread>(digit, live, bits, rounds, counts + warp * digits, place);
         __syncthreads();
-        uint32_t total = 0;
+        // sums over the warps before, eight warps to a thread
+        const int d = threadIdx.x & ((1 << kOneCtaDigit) - 1), part = threadIdx.x >> kOneCtaDigit;
+        if (d < digits) {
+            uint32_t c[kWarps / 4], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps / 4; ++w) c[w] = counts[(part * (kWarps / 4) + w) * digits + d];
+#pragma unroll
+            for (int w = 0; w < kWarps / 4; ++w) {
+                counts[(part * (kWarps / 4) + w) * digits + d] = (uint16_t)sum;
+                sum += c[w];
+            }
+            firsts[part][d] = (uint16_t)sum;
+        }
+        __syncthreads();
+        uint32_t four[4] = {0, 0, 0, 0}, total = 0;
         if ((int)threadIdx.x < digits)
-            for (int w = 0; w < kWarps; ++w) {  // (sums before a warp, in place)
-                const uint32_t c = counts[w * digits + threadIdx.x];
-                counts[w * digits + threadIdx.x] = (uint16_t)total;
-                total += c;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                four[q] = total;
+                total += firsts[q][threadIdx.x];
             }
         const uint32_t base = block_exclusive_sum(total, room);
         if ((int)threadIdx.x < digits)
-            for (int w = 0; w < kWarps; ++w) counts[w * digits + threadIdx.x] = (uint16_t)(counts[w * digits + threadIdx.x] + base);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) firsts[q][threadIdx.x] = (uint16_t)(base + four[q]);
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kOneCtaPerThread; ++r)
             if (live[r]) {
-                const uint32_t d = counts[warp * digits + digit[r]] + place[r];
-                keys[d] = key[r];
-                pos[d] = at[r];
+                const uint32_t to = firsts[warp / (kWarps / 4)][digit[r]] + counts[warp * digits + digit[r]] + place[r];
+                keys[to] = key[r];
+                pos[to] = at[r];
             }
         __syncthreads();
 #pragma unroll
@@ -315,13 +346,15 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const SortArgs a) {
     for (int d = threadIdx.x; d < digits; d += kSortThreads) hist[d] = 0;
     __syncthreads();
     const int64_t lo = (int64_t)blockIdx.x * kSortKeys;
+    uint32_t key[kSortPerThread];
 #pragma unroll
-    for (int r = 0; r < kSortPerThread; ++r) {
-        const int64_t i = lo + r * kSortThreads + threadIdx.x;
-        if (i < a.count) atomicAdd(&hist[(sort_key(a, i) >> a.shift) & (uint32_t)(digits - 1)], 1u);
-    }
+    for (int r = 0; r < kSortPerThread; ++r) key[r] = sort_key(a, min(lo + r * kSortThreads + threadIdx.x, a.count - 1));
+#pragma unroll
+    for (int r = 0; r < kSortPerThread; ++r)
+        if (lo + r * kSortThreads + threadIdx.x < a.count) atomicAdd(&hist[(key[r] >> a.shift) & (uint32_t)(digits - 1)], 1u);
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) a.counts[(int64_t)d * a.blocks + blockIdx.x] = hist[d];
+    for (int d = threadIdx.x; d < digits; d += kSortThreads)
+        a.counts[a.scanned ? (int64_t)d * a.blocks + blockIdx.x : (int64_t)blockIdx.x * digits + d] = hist[d];
 }
 
 // A warp per digit: its counts become sums over the blocks before, its total is noted.
@@ -346,7 +379,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scan(const SortArgs a) {
 }
 
 // Moves the pairs to their places by this pass's digit.
-__global__ void __launch_bounds__(kSortThreads) k_sort_move(const SortArgs a) {
+__global__ void __launch_bounds__(kSortThreads, 2) k_sort_move(const SortArgs a) {
     wait_previous_kernel();
     if ((int)blockIdx.x >= a.blocks) {
         clear_share(a.clear, blockIdx.x - a.blocks, gridDim.x - a.blocks);
@@ -355,12 +388,26 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_move(const SortArgs a) {
     extern __shared__ __align__(16) unsigned char sort_smem[];
     constexpr int kWarps = kSortThreads / 32, kMostPer = (1 << kMaxDigit) / kSortThreads;
     const int digits = 1 << a.bits;
-    uint32_t* base = reinterpret_cast<uint32_t*>(sort_smem);       // [digit] first place of this block's keys
-    uint16_t* counts = reinterpret_cast<uint16_t*>(base + digits); // [warp][digit]
+    uint32_t* keys = reinterpret_cast<uint32_t*>(sort_smem);            // this block's pairs in the order of their digits
+    uint32_t* pos = keys + kSortKeys;
+    uint32_t* base = pos + kSortKeys;                                   // [digit] place of the block's first one, less its place here
+    uint16_t* firsts = reinterpret_cast<uint16_t*>(base + digits);      // [digit] place here of the first one
+    uint16_t* counts = firsts + digits;                                 // [warp][digit]
     __shared__ uint32_t room[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < kWarps * digits; i += kSortThreads) counts[i] = 0;
-    // thread t has the digits from t * per on
+    const int64_t lo = (int64_t)blockIdx.x * kSortKeys + warp * (32 * kSortPerThread);
+    const int here = (int)min((int64_t)kSortKeys, a.count - (int64_t)blockIdx.x * kSortKeys);
+    uint32_t key[kSortPerThread], at[kSortPerThread], digit[kSortPerThread], place[kSortPerThread];
+    bool live[kSortPerThread];
+#pragma unroll
+    for (int r = 0; r < kSortPerThread; ++r) {
+        const int64_t i = lo + 32 * r + lane;
+        live[r] = i < a.count;
+        key[r] = sort_key(a, min(i, a.count - 1));
+        at[r] = a.keys_in ? a.pos_in[min(i, a.count - 1)] : (uint32_t)i;
+    }
+    for (int i = threadIdx.x; i < kWarps * digits / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
+    // thread t has the digits from t * per on: how many there are in all, and in the blocks before this one
     const int per = digits <= kSortThreads ? 1 : digits / kSortThreads;
     uint32_t total[kMostPer], before[kMostPer], sum = 0;
 #pragma unroll
@@ -368,58 +415,66 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_move(const SortArgs a) {
         const int d = threadIdx.x * per + j;
         total[j] = before[j] = 0;
         if (j >= per || d >= digits) continue;
-        const uint32_t* c = a.counts + (int64_t)d * a.blocks;
         if (a.scanned) {
             total[j] = a.totals[d];
-            before[j] = c[blockIdx.x];
+            before[j] = a.counts[(int64_t)d * a.blocks + blockIdx.x];
         } else {
+#pragma unroll 8
             for (int b = 0; b < a.blocks; ++b) {
-                const uint32_t v = c[b];
+                const uint32_t v = a.counts[(int64_t)b * digits + d];
                 total[j] += v;
                 if (b < (int)blockIdx.x) before[j] += v;
             }
         }
         sum += total[j];
     }
-    uint32_t at = block_exclusive_sum(sum, room);
+#pragma unroll
+    for (int r = 0; r < kSortPerThread; ++r) digit[r] = (key[r] >> a.shift) & (uint32_t)(digits - 1);
+    const uint32_t all = block_exclusive_sum(sum, room);
+    __syncthreads();
+    rank_in_warp<kSortPerThread>(digit, live, a.bits, kSortPerThread, counts + warp * digits, place);
+    __syncthreads();
+    // this block's digits: sums over the warps before, then over the digits before
+    uint32_t mine[kMostPer], mine_sum = 0;
+#pragma unroll
+    for (int j = 0; j < kMostPer; ++j) {
+        const int d = threadIdx.x * per + j;
+        mine[j] = 0;
+        if (j >= per || d >= digits) continue;
+        uint32_t c[kWarps];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) c[w] = counts[w * digits + d];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            counts[w * digits + d] = (uint16_t)mine[j];
+            mine[j] += c[w];
+        }
+        mine_sum += mine[j];
+    }
+    uint32_t local = block_exclusive_sum(mine_sum, room), global = all;
 #pragma unroll
     for (int j = 0; j < kMostPer; ++j) {
         const int d = threadIdx.x * per + j;
         if (j >= per || d >= digits) continue;
-        base[d] = at + before[j];
-        at += total[j];
-    }
-    const int64_t lo = (int64_t)blockIdx.x * kSortKeys + warp * (32 * kSortPerThread);
-    uint32_t key[kSortPerThread], digit[kSortPerThread], place[kSortPerThread];
-    bool live[kSortPerThread];
-#pragma unroll
-    for (int r = 0; r < kSortPerThread; ++r) {
-        const int64_t i = lo + 32 * r + lane;
-        live[r] = i < a.count;
-        key[r] = live[r] ? sort_key(a, i) : 0u;
-    }
-#pragma unroll
-    for (int r = 0; r < kSortPerThread; ++r) digit[r] = (key[r] >> a.shift) & (uint32_t)(digits - 1);
-    __syncthreads();
-    rank_in_warp<kSortPerThread>(digit, live, counts + warp * digits, place);
-    __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
-        uint32_t s = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const uint32_t c = counts[w * digits + d];
-            counts[w * digits + d] = (uint16_t)s;
-            s += c;
-        }
+        firsts[d] = (uint16_t)local;
+        base[d] = global + before[j] - local;
+        local += mine[j];
+        global += total[j];
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortPerThread; ++r) {
         if (!live[r]) continue;
-        const int64_t i = lo + 32 * r + lane;
-        const uint32_t to = base[digit[r]] + counts[warp * digits + digit[r]] + place[r];
-        a.keys_out[to] = key[r];
-        a.pos_out[to] = a.keys_in ? a.pos_in[i] : (uint32_t)i;
+        const uint32_t to = firsts[digit[r]] + counts[warp * digits + digit[r]] + place[r];
+        keys[to] = key[r];
+        pos[to] = at[r];
+    }
+    __syncthreads();
+    // neighbouring threads write neighbouring places, digit by digit (pair by pair from where they were read: 80 us for 2.4 M pairs)
+    for (int i = threadIdx.x; i < here; i += kSortThreads) {
+        const uint32_t k = keys[i], to = base[(k >> a.shift) & (uint32_t)(digits - 1)] + i;
+        a.keys_out[to] = k;
+        a.pos_out[to] = pos[i];
     }
 }
 
@@ -818,7 +873,15 @@ extern "C" int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dty
         s.bits = g.digit_bits;
         s.clear.parts = 2 * g.passes;
         const unsigned grid = (unsigned)g.blocks + clear_blocks(s.clear.parts, kSortThreads);
-        const size_t smem = ((size_t)4 + 2 * (kSortThreads / 32)) << g.digit_bits;
+        const size_t smem = 8 * kSortKeys + (((size_t)4 + 2 + 2 * (kSortThreads / 32)) << g.digit_bits);
+        constexpr int kMostSmem = 8 * kSortKeys + ((4 + 2 + 2 * (kSortThreads / 32)) << kMaxDigit);
+        static std::atomic<bool> opted_in[kMaxDevices];
+        int dev = 0;
+        GNNPRE_CUDA(cudaGetDevice(&dev));
+        if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
+            GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_move, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+            if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
+        }
         for (int p = 0; p < g.passes; ++p) {
             s.shift = p * g.digit_bits;
             s.keys_in = p == 0 ? nullptr : pair[at][0];
@@ -829,7 +892,7 @@ extern "C" int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dty
             s.clear.first = 2 * p;
             GNNPRE_TRY(launch_after(k_sort_count, dim3(grid), kSortThreads, 0, p > 0, st, s));
             if (s.scanned)
-                GNNPRE_TRY(launch_after(k_sort_scan, dim3((unsigned)(((1 << g.digit_bits) + 7) / 8)), kSortThreads, 0, true, st, s));
+                GNNPRE_TRY(launch_after(k_sort_scan, dim3((unsigned)(((1 << g.digit_bits) + kSortThreads / 32 - 1) / (kSortThreads / 32))), kSortThreads, 0, true, st, s));
             s.clear.first = 2 * p + 1;
             GNNPRE_TRY(launch_after(k_sort_move, dim3(grid), kSortThreads, smem, true, st, s));
         }
