@@ -379,10 +379,10 @@ _ID_TYPES = {torch.int32: GNNPRE_I32, torch.int64: GNNPRE_I64}
 
 
 def _on_current_device(*tensors) -> None:
-    """The library launches on the current device's stream: operands of another device are refused."""
+    """The library launches on the current device's stream: operands of another device (or of the host: -1) are refused."""
     current = torch.cuda.current_device()
     for t in tensors:
-        assert t.is_cuda and t.get_device() == current
+        assert t.get_device() == current
 
 
 def _rows(t: torch.Tensor) -> int:
@@ -404,15 +404,20 @@ def gnnpre_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: fl
     """scale * table[ids] ([N, D]); an id outside the table (padding) gives a row of zeros.
 
     table: device fp32, bf16 or fp16 [V, D] with stride(1) == 1; ids: device int32 or int64 [N]; out: of table's type."""
-    assert table.dim() == 2 and table.dtype in _DTYPES and ids.dim() == 1 and ids.dtype in _ID_TYPES and ids.is_contiguous()
-    (V, D), N = table.shape, ids.shape[0]
-    assert table.stride(1) == 1 or D == 1
+    V, D = table.shape
+    (N,) = ids.shape
+    dtype, id_type = _DTYPES.get(table.dtype), _ID_TYPES.get(ids.dtype)
+    assert dtype is not None and id_type is not None and ids.is_contiguous()
     if out is None:
         out = torch.empty((N, D), dtype=table.dtype, device=table.device)
-    assert out.dtype is table.dtype and out.shape == (N, D) and (out.stride(1) == 1 or D == 1)
-    _on_current_device(table, ids, out)
-    _check(_lib.gnnpre_embedding_lookup(table.data_ptr(), V, D, _rows(table), _DTYPES[table.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype],
-                                        N, scale, out.data_ptr(), _rows(out), _stream_ptr(stream)), "gnnpre_embedding_lookup")
+    (ldt, one), (ldo, also_one) = table.stride(), out.stride()
+    assert out.dtype is table.dtype and out.shape == (N, D) and (D == 1 or one == 1 == also_one)
+    # (the library launches on the current device's stream: operands of another device, or of the host, are refused)
+    device = torch.cuda.current_device()
+    assert table.get_device() == device == ids.get_device() and out.get_device() == device
+    _check(_lib.gnnpre_embedding_lookup(table.data_ptr(), V, D, ldt if V > 1 else max(ldt, D), dtype, ids.data_ptr(), id_type, N, scale,
+                                        out.data_ptr(), ldo if N > 1 else max(ldo, D),
+                                        _raw_stream(device) if stream is None else stream.cuda_stream), "gnnpre_embedding_lookup")
     return out
 
 
@@ -431,20 +436,22 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
     d_out: device fp32, bf16 or fp16 [N, D]; out: of d_out's type or fp32 (the default).  With accumulate=True it is added to
     out (rows that no id asks for stay untouched).  workspace: uint8 tensor of gnnpre_embedding_grad_workspace bytes, for callers
     that keep one; otherwise one is taken from torch's allocator on the current stream."""
-    assert d_out.dim() == 2 and d_out.dtype in _DTYPES and ids.dim() == 1 and ids.dtype in _ID_TYPES and ids.is_contiguous()
     N, D = d_out.shape
-    assert ids.shape[0] == N and (d_out.stride(1) == 1 or D == 1)
+    dtype, id_type = _DTYPES.get(d_out.dtype), _ID_TYPES.get(ids.dtype)
+    assert dtype is not None and id_type is not None and ids.shape == (N,) and ids.is_contiguous()
     assert out is not None or not accumulate
     if out is None:
         out = torch.empty((num_rows, D), dtype=torch.float32, device=d_out.device)
-    assert out.dtype in (d_out.dtype, torch.float32) and out.shape == (num_rows, D) and (out.stride(1) == 1 or D == 1)
-    _on_current_device(d_out, ids, out)
-    size = _lib.gnnpre_embedding_grad_workspace(num_rows, D, N)
-    room = _workspace(workspace, size, "gnnpre_embedding_grad", d_out.device)
-    _on_current_device(room)
-    _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), _rows(d_out), _DTYPES[d_out.dtype], ids.data_ptr(), _ID_TYPES[ids.dtype], N,
-                                      num_rows, D, scale, int(accumulate), out.data_ptr(), _rows(out), _DTYPES[out.dtype],
-                                      room.data_ptr(), room.numel(), _stream_ptr(stream)), "gnnpre_embedding_grad")
+    (ldd, one), (ldt, also_one) = d_out.stride(), out.stride()
+    to = _DTYPES.get(out.dtype)
+    assert to in (dtype, GNNPRE_F32) and out.shape == (num_rows, D) and (D == 1 or one == 1 == also_one)
+    room = _workspace(workspace, _lib.gnnpre_embedding_grad_workspace(num_rows, D, N), "gnnpre_embedding_grad", d_out.device)
+    device = torch.cuda.current_device()
+    assert d_out.get_device() == device == ids.get_device() and out.get_device() == device == room.get_device()
+    _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), ldd if N > 1 else max(ldd, D), dtype, ids.data_ptr(), id_type, N, num_rows, D, scale,
+                                      int(accumulate), out.data_ptr(), ldt if num_rows > 1 else max(ldt, D), to, room.data_ptr(),
+                                      room.numel(), _raw_stream(device) if stream is None else stream.cuda_stream),
+           "gnnpre_embedding_grad")
     if workspace is None and stream is not None:
         room.record_stream(stream)  # allocated on the current stream, used on another
     return out

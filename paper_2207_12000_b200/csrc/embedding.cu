@@ -516,7 +516,7 @@ __device__ __forceinline__ void store_row(const SumArgs& a, uint32_t row, int64_
     }
 }
 
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 128;
 constexpr int kSumWindow = 8;  // rows in flight per lane
 
 // A group of lanes per segment and E columns per lane; column tiles are the grid's second dimension.
