@@ -137,10 +137,12 @@ struct Clear {
     int32_t wide;                    // 16-byte stores
 };
 
+// The zeros leave the L2 first: kept there, 87 MB of them made room for d_out's rows while those were summed (65,553 rows into
+// 169,343: 63 us a gradient, 51 so).
 __device__ __forceinline__ void clear_bytes(char* p, int64_t bytes, int64_t at, int64_t step, bool wide) {
     if (wide) {
         const int64_t whole = bytes / 16;
-        for (int64_t i = at; i < whole; i += step) reinterpret_cast<uint4*>(p)[i] = make_uint4(0, 0, 0, 0);
+        for (int64_t i = at; i < whole; i += step) __stcs(reinterpret_cast<uint4*>(p) + i, make_uint4(0, 0, 0, 0));
         for (int64_t i = whole * 8 + at; i < bytes / 2; i += step) reinterpret_cast<uint16_t*>(p)[i] = 0;
     } else {
         for (int64_t i = at; i < bytes / 2; i += step) reinterpret_cast<uint16_t*>(p)[i] = 0;
@@ -171,10 +173,11 @@ constexpr int kOneCtaPerThread = 8;
 constexpr int kOneCtaKeys = kOneCtaThreads * kOneCtaPerThread;
 constexpr int kOneCtaDigit = 8;                  // bits
 constexpr int kSortThreads = 512;
-constexpr int kSortPerThread = 8;
-constexpr int kSortKeys = kSortThreads * kSortPerThread;
+// Keys of a block: 2048 (four per thread) while such blocks fit the machine at once, two to an SM, else 4096.  The time of a block is
+// that of its threads' rounds.  us a gradient, 4096 / 2048: 65,553 rows 71 / 63, 300,000 62 / 56, 2.4 M 333 / 342.
+constexpr int kSortFew = 4, kSortMany = 8;
 constexpr int kMaxDigit = 11;
-constexpr int kSelfScanBlocks = 32;              // up to here a block adds up the other blocks' counts itself
+constexpr int kSelfScanBlocks = 64;              // up to here a block adds up the other blocks' counts itself
 
 // Places of one warp's keys among those with the same digit before them in this warp; `counts` is the warp's row of counters.
 // Rounds of 32 neighbouring keys, so the order is kept.  Lanes with the same digit are found bit by bit: the ballots of a round do
@@ -231,7 +234,7 @@ struct SortArgs {
     Ids ids;
     int64_t count;
     int32_t shift, bits;       // of this pass
-    int32_t blocks;            // of kSortKeys keys
+    int32_t blocks;            // of kSortThreads * (kSortFew or kSortMany) keys
     int32_t scanned;           // the counts are sums over the blocks before, `totals` the digits' counts
     const uint32_t* keys_in;   // nullptr: the ids themselves, in their order
     const uint32_t* pos_in;
@@ -335,7 +338,9 @@ __global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) { return a.keys_in ? a.keys_in[i] : id_at(a.ids, i); }
 
 // Digits of each block of keys.
+template <int kSortPerThread>
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(const SortArgs a) {
+    constexpr int kSortKeys = kSortThreads * kSortPerThread;
     wait_previous_kernel();
     if ((int)blockIdx.x >= a.blocks) {
         clear_share(a.clear, blockIdx.x - a.blocks, gridDim.x - a.blocks);
@@ -379,7 +384,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scan(const SortArgs a) {
 }
 
 // Moves the pairs to their places by this pass's digit.
+template <int kSortPerThread>
 __global__ void __launch_bounds__(kSortThreads, 2) k_sort_move(const SortArgs a) {
+    constexpr int kSortKeys = kSortThreads * kSortPerThread;
     wait_previous_kernel();
     if ((int)blockIdx.x >= a.blocks) {
         clear_share(a.clear, blockIdx.x - a.blocks, gridDim.x - a.blocks);
@@ -697,8 +704,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_table_joins(const SumArgs a) {
 
 // ------------------------------------------------------------------------------------------------ host
 
+constexpr int kSortSms = 148;  // (a size that does not depend on the device: the workspace's goes by it)
+
 struct GradShape {
     int32_t key_bits, passes, digit_bits;
+    int32_t per_thread;     // keys of a thread in the sort
     int64_t blocks;         // of the sort
     int32_t length;         // of a segment
     int64_t segments;
@@ -714,7 +724,8 @@ GradShape grad_shape(int64_t n, int64_t dim, int64_t count) {
     while (((int64_t)1 << g.key_bits) <= n) ++g.key_bits;
     g.passes = (g.key_bits + kMaxDigit - 1) / kMaxDigit;
     g.digit_bits = (g.key_bits + g.passes - 1) / g.passes;
-    g.blocks = (count + kSortKeys - 1) / kSortKeys;
+    g.per_thread = count <= (int64_t)2 * kSortSms * kSortThreads * kSortFew ? kSortFew : kSortMany;
+    g.blocks = (count + kSortThreads * g.per_thread - 1) / (kSortThreads * g.per_thread);
     g.length = 8;
     while (g.length < 128 && count / g.length > 8192) g.length *= 2;
     g.segments = (count + g.length - 1) / g.length;
@@ -873,13 +884,16 @@ extern "C" int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dty
         s.bits = g.digit_bits;
         s.clear.parts = 2 * g.passes;
         const unsigned grid = (unsigned)g.blocks + clear_blocks(s.clear.parts, kSortThreads);
-        const size_t smem = 8 * kSortKeys + (((size_t)4 + 2 + 2 * (kSortThreads / 32)) << g.digit_bits);
-        constexpr int kMostSmem = 8 * kSortKeys + ((4 + 2 + 2 * (kSortThreads / 32)) << kMaxDigit);
+        const auto count_keys = g.per_thread == kSortFew ? k_sort_count<kSortFew> : k_sort_count<kSortMany>;
+        const auto move = g.per_thread == kSortFew ? k_sort_move<kSortFew> : k_sort_move<kSortMany>;
+        const size_t smem = 8 * kSortThreads * g.per_thread + (((size_t)4 + 2 + 2 * (kSortThreads / 32)) << g.digit_bits);
+        constexpr int kMostSmem = 8 * kSortThreads * kSortMany + ((4 + 2 + 2 * (kSortThreads / 32)) << kMaxDigit);
         static std::atomic<bool> opted_in[kMaxDevices];
         int dev = 0;
         GNNPRE_CUDA(cudaGetDevice(&dev));
         if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
-            GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_move, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+            GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_move<kSortFew>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
+            GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_move<kSortMany>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem));
             if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
         }
         for (int p = 0; p < g.passes; ++p) {
@@ -890,11 +904,11 @@ extern "C" int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dty
             s.keys_out = pair[at][0];
             s.pos_out = pair[at][1];
             s.clear.first = 2 * p;
-            GNNPRE_TRY(launch_after(k_sort_count, dim3(grid), kSortThreads, 0, p > 0, st, s));
+            GNNPRE_TRY(launch_after(count_keys, dim3(grid), kSortThreads, 0, p > 0, st, s));
             if (s.scanned)
                 GNNPRE_TRY(launch_after(k_sort_scan, dim3((unsigned)(((1 << g.digit_bits) + kSortThreads / 32 - 1) / (kSortThreads / 32))), kSortThreads, 0, true, st, s));
             s.clear.first = 2 * p + 1;
-            GNNPRE_TRY(launch_after(k_sort_move, dim3(grid), kSortThreads, smem, true, st, s));
+            GNNPRE_TRY(launch_after(move, dim3(grid), kSortThreads, smem, true, st, s));
         }
     }
 
