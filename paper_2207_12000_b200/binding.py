@@ -477,45 +477,44 @@ def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor
     K = len(hops)
     shape, hs = hops[0].shape, hops[0].stride()
     n, F = shape
+    device = torch.cuda.current_device()
     assert hs[1] == 1 or F == 1
     for h in hops:
-        assert h.dtype is torch.float32 and h.shape == shape and h.stride() == hs
+        assert h.dtype is torch.float32 and h.shape == shape and h.stride() == hs and h.get_device() == device
     if batch is None:
         N, bptr = n, None
     else:
         if batch.dtype is torch.int64:
             batch = batch.to(torch.int32)
-        assert batch.dtype is torch.int32 and batch.dim() == 1 and batch.is_contiguous()
-        N, bptr = batch.shape[0], batch.data_ptr()
-        _on_current_device(batch)
-    H = dY.shape[-1] // K if concat else dY.shape[-1]
-
-    def layout(t):  # (leading dimension, distance between the hops)
-        assert t.dtype is torch.float32 and t.shape == ((N, K * H) if concat else (K, N, H)) and t.stride(-1) == 1
-        if concat:
-            return _rows(t), H
-        return max(t.stride(1), H) if N <= 1 else t.stride(1), max(t.stride(0), 0)
-
-    lddy, dy_hop = layout(dY)
+        (N,) = batch.shape
+        assert batch.dtype is torch.int32 and batch.is_contiguous() and batch.get_device() == device
+        bptr = batch.data_ptr()
+    last = dY.shape[-1]
+    H = last // K if concat else last
+    want = (N, K * H) if concat else (K, N, H)
+    layout = []  # leading dimension, distance between the hops
+    for t in (dY,) if Y is None else (dY, Y):
+        ts = t.stride()
+        assert t.dtype is torch.float32 and t.shape == want and ts[-1] == 1 and t.get_device() == device
+        ld = ts[-2] if N > 1 else max(ts[-2], want[-1])
+        layout.append((ld, H if concat else ts[0]))
     assert Y is not None or not relu_mask
-    ldy, y_hop = layout(Y) if Y is not None else (0, 0)
+    if Y is None:
+        layout.append((0, 0))
     assert out is not None or not accumulate
     if out is None:
         out = torch.empty((H, F), dtype=torch.float32, device=dY.device)
-    assert out.dtype is torch.float32 and out.shape == (H, F) and (out.stride(1) == 1 or F == 1)
-    _on_current_device(dY, out, *hops)
-    if Y is not None:
-        _on_current_device(Y)
-    size = _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H)
-    room = _workspace(workspace, size, "gnnpre_lc_first_layer_grad", dY.device)
-    _on_current_device(room)
+    ldw, one = out.stride()
+    assert out.dtype is torch.float32 and out.shape == (H, F) and (one == 1 or F == 1) and out.get_device() == device
+    room = _workspace(workspace, _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H), "gnnpre_lc_first_layer_grad", dY.device)
+    assert room.get_device() == device
     flag = torch.zeros(1, dtype=torch.int32, device=dY.device) if check else None
     if check and stream is not None:
         stream.wait_stream(torch.cuda.current_stream())  # the flag is cleared on the current one
-    _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, hs[0], bptr, N, dY.data_ptr(), lddy, dy_hop,
-                                           Y.data_ptr() if Y is not None else None, ldy, y_hop, relu_mask, H, int(accumulate), out.data_ptr(),
-                                           _rows(out), room.data_ptr(), room.numel(), flag.data_ptr() if check else None, _stream_ptr(stream)),
-           "gnnpre_lc_first_layer_grad")
+    _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, hs[0], bptr, N, dY.data_ptr(), *layout[0],
+                                           Y.data_ptr() if Y is not None else None, *layout[1], relu_mask, H, int(accumulate), out.data_ptr(),
+                                           ldw, room.data_ptr(), room.numel(), flag.data_ptr() if check else None,
+                                           _raw_stream(device) if stream is None else stream.cuda_stream), "gnnpre_lc_first_layer_grad")
     if workspace is None and stream is not None:
         room.record_stream(stream)
     if check:

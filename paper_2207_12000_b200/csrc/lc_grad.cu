@@ -42,6 +42,9 @@ constexpr int kGradMaxHops = 8;       // hops per launch
 constexpr int kGradRaw = 6;           // chunks being copied or split
 constexpr int kGradStages = 6;        // chunks split
 constexpr int kGradSlice = 4;         // chunks whose products share an accumulator
+// Of two groups that take chunks in turn each must have its own places of a ring: one that meets a place's barrier only every other
+// phase cannot tell by its parity whether the phase before the awaited one is over.
+static_assert(kGradRaw % 2 == 0 && kGradStages % 2 == 0, "a place belongs to one group");
 constexpr int kGradSumWarps = 8, kGradBWarp = 16, kGradCopyWarp = 24, kGradTileWarp = 26, kGradMmaWarp = 27, kGradWarps = 28;
 constexpr int kGradThreads = 32 * kGradWarps;            // (whole warpgroups, for the registers they hand on)
 constexpr uint32_t kGradAllRows = (1u << kGradChunk) - 1;
@@ -319,7 +322,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
                 if (tc_bar_test(raw_full(t), (uint32_t)((issued - t + kGradRaw - 1) / kGradRaw - 1) & 1u)) break;
     };
     if (warp == kGradCopyWarp || warp == kGradCopyWarp + 1) {
-        static_assert(kGradRaw % 2 == 0, "the warps take places in turn");
         const int w = warp - kGradCopyWarp, n = (int)a.n, rows_in = (int)a.batch_size;
         // This lane's row of the hop matrix in a chunk, -1 or another row outside for none.  Asked for kAhead of the warp's chunks
         // ahead: with one, copies were issued no faster than one load from memory after the other.
