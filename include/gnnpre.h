@@ -482,7 +482,8 @@ int gnnpre_lc_grad_selftest_wait_timeout(const float* hop, int64_t n, int64_t fe
  * with (a, b, c) = coeffs; on G's transpose where G has more rows than columns, which gives the same matrix.
  *
  *   G, out      DEVICE, row-major [rows, cols] of `dtype` (GNNPRE_F32, GNNPRE_BF16, GNNPRE_F16), leading dimensions ldg, ldo;
- *               matrix k begins at G + k * g_stride, out + k * o_stride (elements).  out may be G
+ *               matrix k begins at G + k * g_stride, out + k * o_stride (elements).  out may be G, matrix for matrix; it may not
+ *               overlap G in any other way
  *   coeffs      HOST, three floats.  They must keep the singular values, which start in [0, 1], below 16 in every step, and
  *               |a + b t + c t^2| below 1024 there (else INVALID_ARG)
  *   workspace   DEVICE, 256-byte aligned, gnnpre_orthogonalize_workspace(batch, rows, cols, steps) bytes (which returns a

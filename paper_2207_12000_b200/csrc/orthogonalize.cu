@@ -1305,6 +1305,21 @@ int launch_product(Product& a, int64_t rows, int64_t cols, int64_t batch, bool s
     return narrow ? launch_product_n<64>(a, tiles_m, batch, st) : launch_product_n<128>(a, tiles_m, batch, st);
 }
 
+// Whether a matrix of out lies on one of G that is not its own: matrices are done side by side, so one may be written before another
+// is read.  out may be G itself.
+bool updates_meet(const void* G, int64_t ldg, int64_t g_stride, const void* out, int64_t ldo, int64_t o_stride, int64_t batch, int64_t rows,
+                  int64_t cols, int64_t es) {
+    if (G == out && (ldg == ldo || rows == 1) && (batch == 1 || g_stride == o_stride)) return false;
+    const char *g = static_cast<const char*>(G), *o = static_cast<const char*>(out);
+    if (batch == 1) return arrays_overlap(g, rows, cols, ldg, es, o, rows, cols, ldo, es);
+    const int64_t span = (rows - 1) * std::max(ldg, ldo) + cols;
+    if (!arrays_overlap(g, 1, (batch - 1) * g_stride + span, 1, es, o, 1, (batch - 1) * o_stride + span, 1, es)) return false;
+    if (g_stride != o_stride) return true;
+    for (int64_t k = 1 - batch; k < batch; ++k)  // matrices of one buffer, as many apart
+        if (arrays_overlap(g, rows, cols, ldg, es, o + k * o_stride * es, rows, cols, ldo, es)) return true;
+    return false;
+}
+
 int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_stride, int64_t batch, int32_t dtype, int32_t steps,
               const float* coeffs, float eps, float scale, void* out, int64_t ldo, int64_t o_stride, void* workspace,
               int64_t workspace_bytes, int32_t* error_flag, void* stream, const NsSelfTest* test = nullptr) {
@@ -1323,6 +1338,7 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
     const int64_t span_g = (batch - 1) * g_stride + (rows - 1) * ldg + cols, span_o = (batch - 1) * o_stride + (rows - 1) * ldo + cols;
     if (arrays_overlap(workspace, 1, s.total, 1, 1, G, 1, span_g, 1, es) || arrays_overlap(workspace, 1, s.total, 1, 1, out, 1, span_o, 1, es))
         return GNNPRE_ERR_INVALID_ARG;
+    if (updates_meet(G, ldg, g_stride, out, ldo, o_stride, batch, rows, cols, es)) return GNNPRE_ERR_INVALID_ARG;
     int sms = 0;
     GNNPRE_TRY(device_sms(&sms));
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -160,6 +160,17 @@ def test_batches_strides_and_in_place(B, dtype, shape, pad):
     assert torch.isnan(room[rest]).all()
 
 
+def test_side_by_side_in_one_buffer(B):
+    """G and out as column views of one buffer, and as matrices that alternate in one."""
+    room = torch.zeros((3, 40, 120), device="cuda")
+    room[:, :, :60] = torch.from_numpy(dense((3, 40, 60), 1)).cuda()
+    want = B.gnnpre_orthogonalize(room[:, :, :60].clone())
+    assert torch.equal(B.gnnpre_orthogonalize(room[:, :, :60], out=room[:, :, 60:]), want)
+    turns = torch.zeros((6, 40, 60), device="cuda")
+    turns[::2] = room[:, :, :60]
+    assert torch.equal(B.gnnpre_orthogonalize(turns[::2], out=turns[1::2]), want)
+
+
 def test_zeros_tiny_huge_and_not_finite(B):
     assert (B.gnnpre_orthogonalize(torch.zeros((130, 60), device="cuda")) == 0).all()
     assert torch.isnan(B.gnnpre_orthogonalize(torch.zeros((130, 60), device="cuda"), eps=0.0)).all()

@@ -83,7 +83,11 @@ ORTH = dict(G=0x100000, rows=100, cols=60, ldg=60, g_stride=6000, batch=2, dtype
     (dict(coeffs=coefficients(a=float("nan"))), INVALID_ARG), (dict(coeffs=coefficients(b=float("inf"))), INVALID_ARG),
     (dict(coeffs=coefficients(3.0, 3.0, 3.0)), INVALID_ARG), (dict(coeffs=coefficients(20.0, 0.0, 0.0)), INVALID_ARG),
     (dict(workspace_bytes=1000), INVALID_ARG), (dict(workspace=0x4000080), ALIGN), (dict(G=0x100002), ALIGN), (dict(out=0x400001, dtype=1), ALIGN),
-    (dict(workspace=0x100000), INVALID_ARG), (dict(workspace=0x400000), INVALID_ARG), (dict(batch=0), 0)])
+    (dict(workspace=0x100000), INVALID_ARG), (dict(workspace=0x400000), INVALID_ARG), (dict(batch=0), 0),
+    # out on G, but not matrix for matrix: the next matrix, a row further, another pitch, another distance, a part of it
+    (dict(out=0x100000 + 4 * 6000), INVALID_ARG), (dict(out=0x100000 + 4 * 60), INVALID_ARG), (dict(out=0x100000, ldo=64, o_stride=6400), INVALID_ARG),
+    (dict(out=0x100000, o_stride=7000), INVALID_ARG), (dict(out=0x100000 + 4 * 30, batch=1), INVALID_ARG),
+    (dict(ldg=120, ldo=120, g_stride=12000, o_stride=12000, out=0x100000 + 4 * 59), INVALID_ARG)])
 def test_orthogonalize_refuses(lib, changes, status):
     assert call(lib.gnnpre_orthogonalize, ORTH, **changes) == status
 
