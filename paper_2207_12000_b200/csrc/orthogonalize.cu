@@ -38,6 +38,7 @@ constexpr int kBlockBytes = 2 * kHalfBytes;
 constexpr int kPipeBytes = 192 * 1024;
 constexpr int kSumWarps = 8, kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kProductThreads = 320;
+constexpr int kAccs = 4;                                 // accumulators that take turns
 constexpr int kSliceChunks = 1;                          // chunks of 64 of K in one accumulator
 constexpr int kMaxSteps = 64;
 constexpr float kMostSpectral = 16.f;    // bound of X under which coefficients are accepted
@@ -191,14 +192,17 @@ struct Product {
 // The tensor core cuts, not rounds, a sum that it adds a product to: over K = 4000 in one accumulator the sums of squares in A
 // came out 1e-5 too small (750 additions, half of 2^-23 each).  So an accumulator takes one chunk only, its small terms first, so
 // that four cuts count; two take turns, and their sums are added up in registers, rounded to nearest, while the next ones form.
+// What bounds a wide product is shared memory: per 64 of K a 128 x 128 tile writes 64 KB and the twelve products read 96 KB, 1,280 cycles at
+// 128 bytes a cycle for 840 of the tensor core; 128 x 256 takes 1,920 for twice the work.
 template <int BN>
 __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_constant__ Product a) {
     constexpr uint32_t kBBytes = BN * 128;                  // one part of B's chunk
     constexpr uint32_t kStage = kBlockBytes + 2 * kBBytes;
     constexpr int kStages = kPipeBytes / kStage;
     constexpr int kCols = BN / 2;                           // of a thread
+    constexpr int kTurns = BN == 256 ? 2 : kAccs;           // accumulators that fit tensor memory
     extern __shared__ unsigned char ns_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 5];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 2 * kTurns + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
     volatile int* abort_flag = &abort_word;
@@ -209,8 +213,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
     auto acc_full = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
-    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
-    const uint32_t drained = bar0 + 8u * (2 * kStages + 4);
+    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kStages + kTurns + b); };
+    const uint32_t drained = bar0 + 8u * (2 * kStages + 2 * kTurns);
     const Job& job = a.job[blockIdx.z % a.jobs];
     const int64_t batch = blockIdx.z / a.jobs;
     int bi, bj;  // tile row (of 128), tile column (of BN)
@@ -228,7 +232,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
             tc_bar_init(full(s), 1 + (a.drop ? 1 : 0));
             tc_bar_init(empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kTurns; ++b) {
             tc_bar_init(acc_full(b), 1);
             tc_bar_init(acc_empty(b), kSumWarps);
         }
@@ -236,7 +240,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), 2 * BN);
+    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), kTurns * BN);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -251,20 +255,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
         for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
         const uint32_t taddr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (warp >> 2) * kCols;
         for (int i = 0; i < slices; ++i) {
-            ok = tc_wait_warp(acc_full(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, a.error, a.spin_limit);
+            ok = tc_wait_warp(acc_full(i % kTurns), (uint32_t)(i / kTurns) & 1u, abort_flag, a.error, a.spin_limit);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
             for (int part = 0; part < kCols / 32; ++part) {
                 uint32_t v[32];
-                tc_load32(taddr + (uint32_t)(i & 1) * BN + 32 * part, v);
+                tc_load32(taddr + (uint32_t)(i % kTurns) * BN + 32 * part, v);
                 tc_load_wait();
 #pragma unroll
                 for (int j = 0; j < 32; ++j) sum[32 * part + j] += __uint_as_float(v[j]);
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) tc_bar_arrive(acc_empty(i & 1));
+            if (lane == 0) tc_bar_arrive(acc_empty(i % kTurns));
         }
     } else if (warp == kCopyWarp) {
         if (lane == 0) {
@@ -280,6 +284,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
                 tc_bulk_load(to, job.a.block(batch, bi, kc), kBlockBytes, full(s));
                 if (BN == kBlockRows) {
                     tc_bulk_load(to + kBlockBytes, b, kBlockBytes, full(s));
+                } else if (BN > kBlockRows) {  // two blocks of rows, their high parts behind one another
+#pragma unroll
+                    for (int h = 0; h < BN / kBlockRows; ++h) {
+                        const unsigned char* rows = job.b.block(batch, rb + h, kc);
+                        tc_bulk_load(to + kBlockBytes + h * kHalfBytes, rows, kHalfBytes, full(s));
+                        tc_bulk_load(to + kBlockBytes + kBBytes + h * kHalfBytes, rows + kHalfBytes, kHalfBytes, full(s));
+                    }
                 } else {
                     tc_bulk_load(to + kBlockBytes, b + rows0 * 128, kBBytes, full(s));
                     tc_bulk_load(to + kBlockBytes + kBBytes, b + kHalfBytes + rows0 * 128, kBBytes, full(s));
@@ -308,12 +319,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
         int s = 0;
         uint32_t ph = 0;
         for (int i = 0, kc = 0; i < slices && ok; ++i) {
-            ok = tc_wait_warp(acc_empty(i & 1), ((uint32_t)(i >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
+            ok = tc_wait_warp(acc_empty(i % kTurns), ((uint32_t)(i / kTurns) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit);
             for (int first = kc; ok && kc < min(first + kSliceChunks, job.k_chunks); ++kc) {
                 ok = tc_wait_warp(full(s), ph, abort_flag, a.error, a.spin_limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = base + (uint32_t)s * kStage, d = tmem + (uint32_t)(i & 1) * BN;
+                const uint32_t at = base + (uint32_t)s * kStage, d = tmem + (uint32_t)(i % kTurns) * BN;
                 const uint64_t ah = tc_desc_k(at), al = tc_desc_k(at + kHalfBytes), bh = tc_desc_k(at + kBlockBytes),
                                bl = tc_desc_k(at + kBlockBytes + kBBytes);
 #pragma unroll
@@ -329,7 +340,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
                     ph ^= 1u;
                 }
             }
-            if (ok) tc_commit(acc_full(i & 1));
+            if (ok) tc_commit(acc_full(i % kTurns));
         }
         // tensor memory is freed, and shared memory used again, when the tensor core is done
         tc_commit(drained);
@@ -364,11 +375,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
         // D's blocks of 64 columns lie behind one another in shared memory, then its transpose's blocks of 64 columns (a row of
         // those is a column of the tile); both go out as they lie.
         const bool transposed = job.write_t || (a.symmetric && bi != bj);
-        unsigned char* const tile_t = base_p + BN / kBlockCols * kBlockBytes;
-        for (int form = 0; form < 1 + job.write_2; ++form) {
+        // (a wide tile and its transpose take shared memory one after the other)
+        constexpr bool kApart = 2 * (BN / kBlockCols) * kBlockBytes > kPipeBytes;
+        constexpr uint32_t kTransposed = kApart ? 0u : BN / kBlockCols * kBlockBytes;
+        unsigned char* const tile_t = base_p + kTransposed;
+        const int passes = (1 + job.write_2) * (kApart && transposed ? 2 : 1);
+        for (int pass = 0; pass < passes; ++pass) {
+            const int form = kApart && transposed ? pass / 2 : pass;
+            const bool plain = !kApart || !transposed || pass % 2 == 0, turned = transposed && (!kApart || pass % 2 == 1);
             const Split& to = form ? job.d2 : job.d;
             const float alpha = form ? job.alpha2 : job.alpha, on_diag = form ? job.diag2 : job.diag;
-            if (form) __syncthreads();  // (the first form's copies have read their tiles: thread 0 has waited)
+            if (pass) __syncthreads();  // (the pass before's copies have read their tiles: thread 0 has waited)
             if (warp < kSumWarps)
 #pragma unroll
                 for (int part = 0; part < kCols / 32; ++part) {
@@ -385,9 +402,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
                         uint4 hi, lo;
                         split8(o, hi, lo);
                         unsigned char* d = base_p + c0 / kBlockCols * kBlockBytes + block_byte(row, c0 % kBlockCols + 8 * j);
-                        *reinterpret_cast<uint4*>(d) = hi;
-                        *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
-                        if (transposed) {
+                        if (plain) {
+                            *reinterpret_cast<uint4*>(d) = hi;
+                            *reinterpret_cast<uint4*>(d + kHalfBytes) = lo;
+                        }
+                        if (turned) {
                             const __half* h = reinterpret_cast<const __half*>(&hi);
                             const __half* l = reinterpret_cast<const __half*>(&lo);
 #pragma unroll
@@ -402,29 +421,33 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
             tc_fence_async();
             __syncthreads();
             if (threadIdx.x == 0) {
+                if (plain)
 #pragma unroll
-                for (int b = 0; b < BN / kBlockCols; ++b)
-                    tc_bulk_store(to.block(batch, bi, bj * (BN / kBlockCols) + b), base + b * kBlockBytes, kBlockBytes);
-                if (transposed) {
+                    for (int b = 0; b < BN / kBlockCols; ++b)
+                        tc_bulk_store(to.block(batch, bi, bj * (BN / kBlockCols) + b), base + b * kBlockBytes, kBlockBytes);
+                if (turned) {
                     const Split& to_t = job.write_t ? job.dt : to;
                     const int rows0 = bj * BN % kBlockRows;
-                    const uint32_t from = base + BN / kBlockCols * kBlockBytes;
+                    constexpr uint32_t kPiece = kBBytes < kHalfBytes ? kBBytes : kHalfBytes;  // rows of one block
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        unsigned char* t = to_t.block(batch, bj * BN / kBlockRows, 2 * bi + b) + rows0 * 128;
-                        tc_bulk_store(t, from + b * 2 * kBBytes, kBBytes);
-                        tc_bulk_store(t + kHalfBytes, from + b * 2 * kBBytes + kBBytes, kBBytes);
-                    }
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (uint32_t h = 0; h < kBBytes / kPiece; ++h) {
+                            unsigned char* t = to_t.block(batch, bj * BN / kBlockRows + (int)h, 2 * bi + b) + rows0 * 128;
+                            const uint32_t from = base + kTransposed + b * 2 * kBBytes + h * kPiece;
+                            tc_bulk_store(t, from, kPiece);
+                            tc_bulk_store(t + kHalfBytes, from + kBBytes, kPiece);
+                        }
                 }
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                if (form < job.write_2) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                if (pass + 1 < passes) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 else asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             }
         }
     }
     if (warp == kMmaWarp) {
         tc_fence_after();
-        tc_free(tmem, 2 * BN);
+        tc_free(tmem, kTurns * BN);
     }
 }
 
@@ -476,7 +499,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     constexpr int BN = kClusterTile, kCols = BN / 2;
     constexpr uint32_t kBBytes = BN * 128;
     extern __shared__ unsigned char ns_smem[];
-    __shared__ __align__(8) unsigned long long bars[2 * kClusterStages + 5];
+    __shared__ __align__(8) unsigned long long bars[2 * kClusterStages + 2 * kAccs + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
     __shared__ double room[kProductThreads / 32];
@@ -492,14 +515,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (kClusterStages + s); };
     auto acc_full = [&](int b) { return bar0 + 8u * (2 * kClusterStages + b); };
-    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kClusterStages + 2 + b); };
-    const uint32_t drained = bar0 + 8u * (2 * kClusterStages + 4);
+    auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kClusterStages + kAccs + b); };
+    const uint32_t drained = bar0 + 8u * (2 * kClusterStages + 2 * kAccs);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kClusterStages; ++s) {
             tc_bar_init(full(s), 1 + (a.drop ? 1 : 0));
             tc_bar_init(empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kAccs; ++b) {
             tc_bar_init(acc_full(b), 1);
             tc_bar_init(acc_empty(b), kSumWarps);
         }
@@ -507,7 +530,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), 2 * BN);
+    if (warp == kMmaWarp) tc_alloc(tc_smem(&tmem_slot), kAccs * BN);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -591,17 +614,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
                 for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
                 const int q = warp & 3, half = warp >> 2, row = 32 * q + lane;
                 for (int i = 0; i < k_chunks; ++i, ++chunk) {
-                    ok = ok && tc_wait_warp(acc_full(chunk & 1), (uint32_t)(chunk >> 1) & 1u, abort_flag, a.error, a.spin_limit);
+                    ok = ok && tc_wait_warp(acc_full(chunk % kAccs), (uint32_t)(chunk / kAccs) & 1u, abort_flag, a.error, a.spin_limit);
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t v[32];
-                    tc_load32(tmem + ((uint32_t)(32 * q) << 16) + half * kCols + (uint32_t)(chunk & 1) * BN, v);
+                    tc_load32(tmem + ((uint32_t)(32 * q) << 16) + half * kCols + (uint32_t)(chunk % kAccs) * BN, v);
                     tc_load_wait();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[j] += __uint_as_float(v[j]);
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) tc_bar_arrive(acc_empty(chunk & 1));
+                    if (lane == 0) tc_bar_arrive(acc_empty(chunk % kAccs));
                 }
                 if (last) {
                     if (!ok) continue;
@@ -699,11 +722,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
             } else {
                 for (int kc = 0; kc < k_chunks && ok; ++kc) {
                     const int s = chunk % kClusterStages;
-                    ok = tc_wait_warp(acc_empty(chunk & 1), ((uint32_t)(chunk >> 1) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit) &&
+                    ok = tc_wait_warp(acc_empty(chunk % kAccs), ((uint32_t)(chunk / kAccs) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit) &&
                          tc_wait_warp(full(s), (uint32_t)(chunk / kClusterStages) & 1u, abort_flag, a.error, a.spin_limit);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t at = base + (uint32_t)s * kClusterStage, d = tmem + (uint32_t)(chunk & 1) * BN;
+                    const uint32_t at = base + (uint32_t)s * kClusterStage, d = tmem + (uint32_t)(chunk % kAccs) * BN;
                     const uint64_t ah = tc_desc_k(at), al = tc_desc_k(at + kHalfBytes), bh = tc_desc_k(at + kBlockBytes),
                                    bl = tc_desc_k(at + kBlockBytes + kBBytes);
 #pragma unroll
@@ -714,7 +737,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
 #pragma unroll
                     for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(d, ah + 2 * j, bh + 2 * j, instr, 1u);
                     tc_commit(empty(s));
-                    tc_commit(acc_full(chunk & 1));
+                    tc_commit(acc_full(chunk % kAccs));
                     ++chunk;
                 }
             }
@@ -745,7 +768,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     __syncthreads();
     if (warp == kMmaWarp) {
         tc_fence_after();
-        tc_free(tmem, 2 * BN);
+        tc_free(tmem, kAccs * BN);
     }
 }
 
@@ -1301,7 +1324,10 @@ int launch_product(Product& a, int64_t rows, int64_t cols, int64_t batch, bool s
     // Tiles of 128 x 64 while they fit the machine; symmetric products need square ones to leave any out.
     const bool narrow = tiles_m * (cols / 64) * batch * a.jobs <= sms;
     a.symmetric = symmetric && !narrow && tiles_m > 1;
-    a.tiles_n = (int32_t)(narrow ? cols / 64 : cols / 128);
+    // Tiles of 128 x 256 where they give every SM one (2,048 x 4,096, five steps: 1,340 us without them, 1,216 with).
+    const bool wide = !narrow && !a.symmetric && cols % 256 == 0 && tiles_m * (cols / 256) * batch * a.jobs >= sms;
+    a.tiles_n = (int32_t)(narrow ? cols / 64 : wide ? cols / 256 : cols / 128);
+    if (wide) return launch_product_n<256>(a, tiles_m, batch, st);
     return narrow ? launch_product_n<64>(a, tiles_m, batch, st) : launch_product_n<128>(a, tiles_m, batch, st);
 }
 

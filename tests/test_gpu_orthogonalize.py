@@ -53,8 +53,11 @@ SHAPES = [(1, 1), (1, 7), (9, 1), (16, 16), (100, 37), (128, 128), (129, 130), (
           (500, 2000), (1000, 777), (1300, 1290), (2048, 384)]
 
 
+LARGE = [(1750, 2800), (2800, 1750), (2040, 2048)]  # products whose tiles fill the machine at twice the width
+
+
 @pytest.mark.parametrize("coeffs,steps", [(QUINTIC, 5), (QUINTIC, 4), (QUINTIC, 1), (CUBIC, 7), (SLOW, 2)])
-@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("rows,cols", SHAPES + LARGE)
 def test_one_value_per_row_and_column(B, rows, cols, coeffs, steps):
     rng = np.random.default_rng(rows * 7 + cols)
     r = min(rows, cols)
@@ -122,6 +125,28 @@ def test_dense(B, dtype, shape):
     plain = plain_f32(G.mT if tall else G, steps, c, 1e-7, scale)
     plain = wide(plain.mT if tall else plain)
     assert err <= 8 * np.linalg.norm(plain - want) + rounding + 2.0 ** -20 * np.linalg.norm(want), (err, np.linalg.norm(plain - want))
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16, F16))
+@pytest.mark.parametrize("shape", LARGE)
+def test_large_dense(B, shape, dtype):
+    """The same comparison with plain fp32 as above, both against the recurrence in 64 bits on the device; steps that 16-bit outputs
+    multiply together are off by no more than in test_steps_that_are_multiplied_together."""
+    G = torch.from_numpy(dense(shape, 8)).cuda().to(dtype)
+    c = f32(QUINTIC)
+    X = G.double() / (G.double().square().sum().sqrt() + float(np.float32(1e-7)))
+    tall = shape[0] > shape[1]
+    X = X.mT if tall else X
+    for _ in range(5):
+        A = X @ X.mT
+        X = c[0] * X + (c[1] * A + c[2] * (A @ A)) @ X
+    want = X.mT if tall else X
+    plain = plain_f32(G.mT if tall else G, 5, c, 1e-7, 1.0)
+    plain = plain.mT if tall else plain
+    got = B.gnnpre_orthogonalize(G)
+    carried = {F32: 0.0, BF16: 2 * 2.0 ** -11, F16: 3 * 2.0 ** -14}[dtype]
+    bound = 8 * (plain.double() - want).norm() + (2.0 ** -20 + carried + torch.finfo(dtype).eps / 2) * want.norm()
+    assert float((got.double() - want).norm()) <= float(bound)
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
