@@ -90,25 +90,36 @@ struct Source {
     Split x, xt;
 };
 
-constexpr int kNormBlocks = 64;
+constexpr int kNormBlocks = 256;
 constexpr int kNormThreads = 256;
 
-__device__ __forceinline__ float source_at(const Source& s, int64_t batch, int64_t i, int64_t j) {
-    const int64_t at = batch * s.batch_stride + i * s.ldg + j;
-    if (s.dtype == GNNPRE_F32) return static_cast<const float*>(s.g)[at];
-    if (s.dtype == GNNPRE_BF16) return to_f32(static_cast<const __nv_bfloat16*>(s.g)[at]);
-    return to_f32(static_cast<const __half*>(s.g)[at]);
+// f with G as what it is.
+template <typename F>
+__device__ __forceinline__ void with_type(const Source& s, int64_t batch, F f) {
+    const int64_t at = batch * s.batch_stride;
+    if (s.dtype == GNNPRE_F32) f(static_cast<const float*>(s.g) + at);
+    else if (s.dtype == GNNPRE_BF16) f(static_cast<const __nv_bfloat16*>(s.g) + at);
+    else f(static_cast<const __half*>(s.g) + at);
 }
 
 // Squares in 64 bits: neither tiny nor huge updates lose their norm.
 __global__ void __launch_bounds__(kNormThreads) k_ns_norm(const Source s) {
     __shared__ double room[kNormThreads / 32];
     double sum = 0;
-    for (int64_t i = blockIdx.x; i < s.rows; i += gridDim.x)
-        for (int64_t j = threadIdx.x; j < s.cols; j += kNormThreads) {
-            const double v = source_at(s, blockIdx.y, i, j);
-            sum += v * v;
+    with_type(s, blockIdx.y, [&](const auto* g) {
+        for (int64_t i = blockIdx.x; i < s.rows; i += gridDim.x) {
+            // (what lies beyond a row's end is its last element again, so that the loads do not wait for a condition)
+            constexpr int kAtOnce = 8;
+            for (int j0 = threadIdx.x; j0 < s.cols; j0 += kAtOnce * kNormThreads) {
+                float v[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) v[u] = to_f32(g[i * s.ldg + min(j0 + u * kNormThreads, s.cols - 1)]);
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (j0 + u * kNormThreads < s.cols) sum += (double)v[u] * v[u];
+            }
         }
+    });
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = sum;
@@ -121,24 +132,33 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_norm(const Source s) {
 
 // X and its transpose, split: a CTA takes [64, 64] of X.
 __global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t norm_blocks) {
-    wait_previous_kernel();
     __shared__ float tile[64][65];
     __shared__ double inverse;
     const int64_t batch = blockIdx.z;
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;  // of X
-    if (threadIdx.x == 0) {
+    const int fast = threadIdx.x & 63, gi0 = (s.tall ? j0 : i0) + (threadIdx.x >> 6), gj = (s.tall ? i0 : j0) + fast;
+    // neighbouring threads, neighbouring elements of G (nothing before this kernel writes them)
+    float v[16];
+    with_type(s, batch, [&](const auto* g) {
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = to_f32(g[(int64_t)min(gi0 + 4 * u, s.rows - 1) * s.ldg + min(gj, s.cols - 1)]);
+    });
+    wait_previous_kernel();
+    if (threadIdx.x < 32) {  // the blocks' sums in a fixed order
         double sum = 0;
-        for (int b = 0; b < norm_blocks; ++b) sum += s.partial[batch * kNormBlocks + b];
-        inverse = 1.0 / (sqrt(sum) + s.eps);
+        for (int b = threadIdx.x; b < norm_blocks; b += 32) sum += s.partial[batch * kNormBlocks + b];
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (threadIdx.x == 0) inverse = 1.0 / (sqrt(sum) + s.eps);
     }
     __syncthreads();
     const double scale = inverse * (double)s.factor;
-    const int fast = threadIdx.x & 63;
-    for (int slow = threadIdx.x >> 6; slow < 64; slow += 4) {
-        const int gi = (s.tall ? j0 : i0) + slow, gj = (s.tall ? i0 : j0) + fast;  // neighbouring threads, neighbouring elements of G
-        const float v = gi < s.rows && gj < s.cols ? (float)((double)source_at(s, batch, gi, gj) * scale) : 0.f;
-        if (s.tall) tile[fast][slow] = v;
-        else tile[slow][fast] = v;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+        const int slow = (threadIdx.x >> 6) + 4 * u;
+        const float o = gi0 + 4 * u < s.rows && gj < s.cols ? (float)((double)v[u] * scale) : 0.f;
+        if (s.tall) tile[fast][slow] = o;
+        else tile[slow][fast] = o;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 64 * 8; c += 256) {
@@ -544,13 +564,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     for (int t = rank, k = 0; t < tiles; t += ctas, ++k) {
         const int i0 = t / side_tiles * 64, j0 = t % side_tiles * 64, fast = threadIdx.x & 63;
         if (warp >= kSumWarps) continue;
+        const int gi0 = (src.tall ? j0 : i0) + (threadIdx.x >> 6), gj = (src.tall ? i0 : j0) + fast;
+        float v[16];
+        with_type(src, batch, [&](const auto* g) {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = to_f32(g[(int64_t)min(gi0 + 4 * u, src.rows - 1) * src.ldg + min(gj, src.cols - 1)]);
+        });
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
             const int slow = (threadIdx.x >> 6) + 4 * u;
-            const int gi = (src.tall ? j0 : i0) + slow, gj = (src.tall ? i0 : j0) + fast;
-            const float v = gi < src.rows && gj < src.cols ? source_at(src, batch, gi, gj) : 0.f;
-            tile[k][src.tall ? fast : slow][src.tall ? slow : fast] = v;
-            sum2 += (double)v * v;
+            const float o = gi0 + 4 * u < src.rows && gj < src.cols ? v[u] : 0.f;
+            tile[k][src.tall ? fast : slow][src.tall ? slow : fast] = o;
+            sum2 += (double)o * o;
         }
     }
 #pragma unroll
