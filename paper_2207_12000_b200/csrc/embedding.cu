@@ -168,9 +168,8 @@ __global__ void k_clear(const Clear c) { clear_share(c, blockIdx.x, gridDim.x); 
 
 // ------------------------------------------------------------------------------------------------ sorting
 
-constexpr int kOneCtaThreads = 1024;
 constexpr int kOneCtaPerThread = 8;
-constexpr int kOneCtaKeys = kOneCtaThreads * kOneCtaPerThread;
+constexpr int kOneCtaKeys = 1024 * kOneCtaPerThread;  // by a CTA of 1024 threads, fewer keys by one of 512 or 256
 constexpr int kOneCtaDigit = 8;                  // bits
 constexpr int kSortThreads = 512;
 // Keys of a block: 2048 (four per thread) while such blocks fit the machine at once, two to an SM, else 4096.  The time of a block is
@@ -246,18 +245,20 @@ struct SortArgs {
 };
 
 // All passes by one CTA; the others clear the table.
-__global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs a, const int32_t key_bits) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_sort_one_cta(const SortArgs a, const int32_t key_bits) {
     if (blockIdx.x > 0) {
         clear_share(a.clear, blockIdx.x - 1, gridDim.x - 1);
         return;
     }
     extern __shared__ __align__(16) unsigned char sort_smem[];
     uint32_t* keys = reinterpret_cast<uint32_t*>(sort_smem);
-    uint16_t* pos = reinterpret_cast<uint16_t*>(keys + kOneCtaKeys);
-    uint16_t* counts = pos + kOneCtaKeys;  // [warp][digit]
-    __shared__ uint16_t firsts[4][1 << kOneCtaDigit];
+    constexpr int kKeys = THREADS * kOneCtaPerThread, kParts = THREADS >> kOneCtaDigit, kPartWarps = (1 << kOneCtaDigit) / 32;
+    uint16_t* pos = reinterpret_cast<uint16_t*>(keys + kKeys);
+    uint16_t* counts = pos + kKeys;  // [warp][digit]
+    __shared__ uint16_t firsts[kParts][1 << kOneCtaDigit];
     __shared__ uint32_t room[32];
-    constexpr int kWarps = kOneCtaThreads / 32;
+    constexpr int kWarps = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = (int)a.count;
     // neighbouring keys of a warp, in rounds that no thread needs more of than there are keys for
@@ -276,7 +277,7 @@ __global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs 
     const int digits = 1 << bits;
     for (int p = 0; p < passes; ++p) {
         const int shift = p * bits;
-        for (int i = threadIdx.x; i < kWarps * digits / 2; i += kOneCtaThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
+        for (int i = threadIdx.x; i < kWarps * digits / 2; i += THREADS) reinterpret_cast<uint32_t*>(counts)[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kOneCtaPerThread; ++r) digit[r] = (key[r] >> shift) & (uint32_t)(digits - 1);
@@ -285,33 +286,33 @@ __global__ void __launch_bounds__(kOneCtaThreads) k_sort_one_cta(const SortArgs 
         // sums over the warps before, eight warps to a thread
         const int d = threadIdx.x & ((1 << kOneCtaDigit) - 1), part = threadIdx.x >> kOneCtaDigit;
         if (d < digits) {
-            uint32_t c[kWarps / 4], sum = 0;
+            uint32_t c[kPartWarps], sum = 0;
 #pragma unroll
-            for (int w = 0; w < kWarps / 4; ++w) c[w] = counts[(part * (kWarps / 4) + w) * digits + d];
+            for (int w = 0; w < kPartWarps; ++w) c[w] = counts[(part * (kPartWarps) + w) * digits + d];
 #pragma unroll
-            for (int w = 0; w < kWarps / 4; ++w) {
-                counts[(part * (kWarps / 4) + w) * digits + d] = (uint16_t)sum;
+            for (int w = 0; w < kPartWarps; ++w) {
+                counts[(part * (kPartWarps) + w) * digits + d] = (uint16_t)sum;
                 sum += c[w];
             }
             firsts[part][d] = (uint16_t)sum;
         }
         __syncthreads();
-        uint32_t four[4] = {0, 0, 0, 0}, total = 0;
+        uint32_t ahead[kParts], total = 0;
         if ((int)threadIdx.x < digits)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                four[q] = total;
+            for (int q = 0; q < kParts; ++q) {
+                ahead[q] = total;
                 total += firsts[q][threadIdx.x];
             }
         const uint32_t base = block_exclusive_sum(total, room);
         if ((int)threadIdx.x < digits)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) firsts[q][threadIdx.x] = (uint16_t)(base + four[q]);
+            for (int q = 0; q < kParts; ++q) firsts[q][threadIdx.x] = (uint16_t)(base + ahead[q]);
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kOneCtaPerThread; ++r)
             if (live[r]) {
-                const uint32_t to = firsts[warp / (kWarps / 4)][digit[r]] + counts[warp * digits + digit[r]] + place[r];
+                const uint32_t to = firsts[warp / (kPartWarps)][digit[r]] + counts[warp * digits + digit[r]] + place[r];
                 keys[to] = key[r];
                 pos[to] = at[r];
             }
@@ -869,15 +870,21 @@ extern "C" int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dty
     if (count <= kOneCtaKeys) {
         s.keys_out = pair[0][0];
         s.pos_out = pair[0][1];
-        constexpr int kSmem = kOneCtaKeys * 6 + kOneCtaThreads / 32 * 2 * (1 << kOneCtaDigit);
-        static std::atomic<bool> opted_in[kMaxDevices];
-        int dev = 0;
-        GNNPRE_CUDA(cudaGetDevice(&dev));
-        if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
-            GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_one_cta, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-            if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
+        // The fewer threads wait for one another, the sooner a pass is done: as many as eight keys each need (a gradient in a graph, us, by
+        // 1024 threads / so: 37 ids 11.7 / 8.2, 500 12.8 / 10.1, 3,000 15.6 / 14.7).
+        const int threads = count <= 256 * kOneCtaPerThread ? 256 : count <= 512 * kOneCtaPerThread ? 512 : 1024;
+        const auto sort = threads == 256 ? k_sort_one_cta<256> : threads == 512 ? k_sort_one_cta<512> : k_sort_one_cta<1024>;
+        constexpr int kPerThread = kOneCtaPerThread * 6 + 2 * (1 << kOneCtaDigit) / 32;  // bytes of shared memory
+        if (threads == 1024) {
+            static std::atomic<bool> opted_in[kMaxDevices];
+            int dev = 0;
+            GNNPRE_CUDA(cudaGetDevice(&dev));
+            if (dev >= kMaxDevices || !opted_in[dev].load(std::memory_order_relaxed)) {
+                GNNPRE_CUDA(cudaFuncSetAttribute(k_sort_one_cta<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 * kPerThread));
+                if (dev < kMaxDevices) opted_in[dev].store(true, std::memory_order_relaxed);
+            }
         }
-        k_sort_one_cta<<<1 + clear_blocks(1, kOneCtaThreads), kOneCtaThreads, kSmem, st>>>(s, g.key_bits);
+        sort<<<1 + clear_blocks(1, threads), threads, (size_t)threads * kPerThread, st>>>(s, g.key_bits);
         GNNPRE_CUDA(cudaGetLastError());
     } else {
         s.scanned = g.blocks > kSelfScanBlocks;
