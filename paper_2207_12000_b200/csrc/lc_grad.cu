@@ -24,9 +24,11 @@
 // scale fits; of the nine products the six largest are taken, which drops less than 2^-23 of |dZ||X| per term.  (Two fp16 numbers
 // and three products would need a scale known before the data is read.)
 //
-// Tensor memory: two accumulators of 128 columns in turn, then 48 columns (three parts of 16: two elements of K per column) for each
-// of five chunks of A.  What A takes there it neither writes to nor is read from shared memory, whose bandwidth B alone then
-// needs.
+// Tensor memory: two accumulators of 128 columns in turn, then 24 columns (three parts of 8: two elements of K per column) for each of
+// six chunks of A.  What A takes there it neither writes to nor is read from shared memory, whose bandwidth B alone then needs.
+//
+// Measured: 2.4 M rows x 3 hops, F = 100, hidden 256: 4.35 ms in long runs (3.6 TB/s, 55 % of the copy rate; 3.7 ms on a cool device),
+// 7.35 M rows' products at 86 TFLOP/s, six times that on the tensor cores.  A chunk takes some 1,000 cycles, its products 384.
 #include <algorithm>
 #include <atomic>
 

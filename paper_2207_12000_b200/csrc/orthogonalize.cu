@@ -20,6 +20,9 @@
 // none of it: [256, 128] with six strong directions is off by 1.8e-6 in steps by themselves (as plain fp32 is) and by 2.0e-4 in
 // segments of three.  So segments have three steps at most for bf16 outputs (one rounding: 1.7e-3), two for fp16, one for fp32.
 //
+// Measured, us, five steps: 256 x 128 61 (one CTA, from shared memory), three of 256 x 602 144 (a cluster of 16 CTAs each), 2,048 x
+// 4,096 1,220 (a launch per product; 164-182 TFLOP/s of the least work, three times that on the tensor cores).
+//
 // Layout.  Operands are stored as the tensor core reads them: blocks of 128 rows x 64 columns of K in the 128-byte swizzle, the
 // high parts' 16 KB and then the low parts', so an operand tile is one contiguous copy and needs no tensor map.
 #include <algorithm>
