@@ -330,6 +330,11 @@ def gnnpre_propagate_weighted(plan: Plan, X: torch.Tensor, gamma, *, out=None, Z
 GNNPRE_LC_TF32, GNNPRE_LC_TF32X3 = 0, 1
 
 
+def _int32_rows(batch: torch.Tensor, n: int) -> torch.Tensor:
+    """int64 row indices as the library takes them: what lies outside [0, n) still does (2^32 + 5 is not row 5)."""
+    return batch.clamp(-1, n).to(torch.int32)
+
+
 def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, precision: int = GNNPRE_LC_TF32,
                           out: torch.Tensor | None = None,
                           concat: bool = False, check: bool = True, stream=None) -> torch.Tensor:
@@ -351,7 +356,7 @@ def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, 
         B, bptr = n, None
     else:
         if batch.dtype is torch.int64:  # the default index type of the host framework; the library takes int32
-            batch = batch.to(torch.int32)
+            batch = _int32_rows(batch, n)
         assert batch.is_cuda and batch.dtype is torch.int32 and batch.dim() == 1 and batch.is_contiguous()
         B, bptr = batch.shape[0], batch.data_ptr()
     if out is None:
@@ -485,7 +490,7 @@ def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor
         N, bptr = n, None
     else:
         if batch.dtype is torch.int64:
-            batch = batch.to(torch.int32)
+            batch = _int32_rows(batch, n)
         (N,) = batch.shape
         assert batch.dtype is torch.int32 and batch.is_contiguous() and batch.get_device() == device
         bptr = batch.data_ptr()

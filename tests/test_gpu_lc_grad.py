@@ -214,3 +214,14 @@ def test_a_training_step_of_the_first_stage(B):
     slope = float(lin(table + D) - lin(table - D)) / 2
     assert abs(slope - float((d_table.double() * D[:, :32].double()).sum())) <= 1e-4 * abs(slope)
     plan.close()
+
+
+def test_int64_indices_beyond_32_bits_are_padding(B):
+    """2^32 + 5 and the like name no row, whatever their lower half is."""
+    rng = np.random.default_rng(9)
+    n, F, H = 50, 20, 32
+    hop = rng.integers(-3, 4, size=(n, F)).astype(np.float32)
+    batch = np.array([3, (1 << 32) + 5, 7, -(1 << 32) + 2, (1 << 33), -(1 << 40), 49, 50, -1, np.iinfo(np.int64).max, np.iinfo(np.int64).min])
+    dY = rng.integers(-3, 4, size=(1, batch.size, H)).astype(np.float32)
+    got = B.gnnpre_lc_first_layer_grad([aligned(hop)], torch.from_numpy(batch).cuda(), torch.from_numpy(dY).cuda())
+    assert np.array_equal(got.cpu().double().numpy(), orc.lc_first_layer_grad([hop], batch, dY, None, 0))

@@ -258,3 +258,13 @@ def test_waits_of_the_split_operand_kernels_that_run_out_are_reported(B, n, F, H
             Y = B.gnnpre_lc_first_layer(hops, batch, Wt, precision=precision)
             want = orc.lc_first_layer(hops_np[0], None if bs is None else batch.cpu().numpy(), Wt_np, relu=False)
             assert np.array_equal(to_np(Y[0]).astype(np.float64), want)
+
+
+def test_int64_indices_beyond_32_bits_are_padding(B):
+    """2^32 + 5 and the like name no row, whatever their lower half is: their outputs are those of a row of zeros."""
+    hop = torch.ones((50, 20), device="cuda")
+    Wt = torch.ones((32, 20), device="cuda")
+    batch = torch.tensor([3, (1 << 32) + 5, 7, -(1 << 32) + 2, 1 << 33, -(1 << 40), 49, 50, -1], device="cuda")
+    for precision in (B.GNNPRE_LC_TF32, B.GNNPRE_LC_TF32X3):
+        Y = B.gnnpre_lc_first_layer([hop], batch, Wt, precision=precision)
+        assert Y[0, :, 0].tolist() == [20, 0, 20, 0, 0, 0, 20, 0, 0]
