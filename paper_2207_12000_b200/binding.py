@@ -3,9 +3,13 @@
 Only argument marshalling happens here.  Tensors are torch tensors used as plain device (or
 host) memory; every step of the computation runs inside the library's CUDA kernels.  If the
 library has not been built, importing this module raises: there is no fallback.
+
+`stream` (default: the current one) is where a call's kernels run.  What the caller brings is ordered with it by the caller; a call that
+makes its result itself, checks its waits or converts indices has it wait for the current stream first.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Sequence
@@ -153,6 +157,42 @@ def _stream_ptr(stream) -> int:
     return stream.cuda_stream
 
 
+def _on(stream):
+    """Where a call takes and fills what it makes for itself (workspace, converted indices, error word): on the stream that its kernels
+    run on, whose order then covers a block from its last use to its next."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _wait_for_current(stream) -> None:
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+
+
+def _result(shape, dtype, device, stream) -> torch.Tensor:
+    """A result that the caller did not bring, from the current stream's memory.  If the kernels run on another stream, that one waits for
+    the current one, whose work may still use the block, and the allocator is told of the use there."""
+    out = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        _wait_for_current(stream)
+        out.record_stream(stream)
+    return out
+
+
+def _error_word(device, stream) -> torch.Tensor:
+    """Of a checked call, which runs after what the current stream has been given."""
+    _wait_for_current(stream)
+    with _on(stream):
+        return torch.zeros(1, dtype=torch.int32, device=device)
+
+
+def _check_waits(flag: torch.Tensor, stream, where: str) -> None:
+    """Synchronises with the call that was given `flag` and raises if a wait of it ran out."""
+    with _on(stream):
+        ran_out = int(flag.item()) != 0
+    if ran_out:
+        raise GnnpreError(-8, where)
+
+
 def _pointers(tensors):
     return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
 
@@ -297,8 +337,8 @@ def gnnpre_lc_selftest_wait_timeout(hop: torch.Tensor, Wt: torch.Tensor, polls: 
     """Status of a first-layer launch whose waits are made to run out (expected: -8, GNNPRE_ERR_TIMEOUT)."""
     n, F = hop.shape
     H = Wt.shape[0]
-    Y = torch.empty((min(n, 128), H), dtype=torch.float32, device=hop.device)
-    flag = torch.zeros(1, dtype=torch.int32, device=hop.device)
+    Y = _result((min(n, 128), H), torch.float32, hop.device, stream)
+    flag = _error_word(hop.device, stream)
     return int(_lib.gnnpre_lc_selftest_wait_timeout(hop.data_ptr(), n, F, hop.stride(0), Wt.data_ptr(), H, Wt.stride(0),
                                                     Y.data_ptr(), Y.stride(0), flag.data_ptr(), polls, _stream_ptr(stream)))
 
@@ -330,9 +370,11 @@ def gnnpre_propagate_weighted(plan: Plan, X: torch.Tensor, gamma, *, out=None, Z
 GNNPRE_LC_TF32, GNNPRE_LC_TF32X3 = 0, 1
 
 
-def _int32_rows(batch: torch.Tensor, n: int) -> torch.Tensor:
+def _int32_rows(batch: torch.Tensor, n: int, stream) -> torch.Tensor:
     """int64 row indices as the library takes them: what lies outside [0, n) still does (2^32 + 5 is not row 5)."""
-    return batch.clamp(-1, n).to(torch.int32)
+    _wait_for_current(stream)
+    with _on(stream):
+        return batch.clamp(-1, n).to(torch.int32)
 
 
 def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, precision: int = GNNPRE_LC_TF32,
@@ -356,11 +398,11 @@ def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, 
         B, bptr = n, None
     else:
         if batch.dtype is torch.int64:  # the default index type of the host framework; the library takes int32
-            batch = _int32_rows(batch, n)
+            batch = _int32_rows(batch, n, stream)
         assert batch.is_cuda and batch.dtype is torch.int32 and batch.dim() == 1 and batch.is_contiguous()
         B, bptr = batch.shape[0], batch.data_ptr()
     if out is None:
-        out = torch.empty((B, K * H) if concat else (K, B, H), dtype=torch.float32, device=Wt.device)
+        out = _result((B, K * H) if concat else (K, B, H), torch.float32, Wt.device, stream)
     os = out.stride()
     if concat:
         assert out.shape == (B, K * H) and os[1] == 1
@@ -368,12 +410,12 @@ def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, 
     else:
         assert out.shape == (K, B, H) and os[2] == 1
         ldy, hop_stride = (os[1], os[0]) if B > 0 else (H, 0)
-    flag = torch.zeros(1, dtype=torch.int32, device=Wt.device) if check else None
+    flag = _error_word(Wt.device, stream) if check else None
     _check(_lib.gnnpre_lc_first_layer(_pointers(hops), K, n, F, hs[0], bptr, B, Wt.data_ptr(), H, ws[0],
                                       relu_mask, precision, out.data_ptr(), ldy, hop_stride,
                                       flag.data_ptr() if check else None, _stream_ptr(stream)), "gnnpre_lc_first_layer")
-    if check and int(flag.item()) != 0:
-        raise GnnpreError(-8, "gnnpre_lc_first_layer")
+    if check:
+        _check_waits(flag, stream, "gnnpre_lc_first_layer")
     return out
 
 
@@ -390,16 +432,12 @@ def _on_current_device(*tensors) -> None:
         assert t.get_device() == current
 
 
-def _rows(t: torch.Tensor) -> int:
-    """Leading dimension of a row-major matrix (a matrix of one row or none may have any)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _workspace(given: torch.Tensor | None, size: int, where: str, device) -> torch.Tensor:
+def _workspace(given: torch.Tensor | None, size: int, where: str, device, stream) -> torch.Tensor:
     if size < 0:
         raise GnnpreError(size, where)
     if given is None:
-        return torch.empty(size, dtype=torch.uint8, device=device)
+        with _on(stream):
+            return torch.empty(size, dtype=torch.uint8, device=device)
     assert given.dtype is torch.uint8 and given.is_contiguous() and given.numel() >= size
     return given
 
@@ -414,7 +452,7 @@ def gnnpre_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: fl
     dtype, id_type = _DTYPES.get(table.dtype), _ID_TYPES.get(ids.dtype)
     assert dtype is not None and id_type is not None and ids.is_contiguous()
     if out is None:
-        out = torch.empty((N, D), dtype=table.dtype, device=table.device)
+        out = _result((N, D), table.dtype, table.device, stream)
     (ldt, one), (ldo, also_one) = table.stride(), out.stride()
     assert out.dtype is table.dtype and out.shape == (N, D) and (D == 1 or one == 1 == also_one)
     # (the library launches on the current device's stream: operands of another device, or of the host, are refused)
@@ -440,25 +478,23 @@ def gnnpre_embedding_grad(d_out: torch.Tensor, ids: torch.Tensor, num_rows: int,
 
     d_out: device fp32, bf16 or fp16 [N, D]; out: of d_out's type or fp32 (the default).  With accumulate=True it is added to
     out (rows that no id asks for stay untouched).  workspace: uint8 tensor of gnnpre_embedding_grad_workspace bytes, for callers
-    that keep one; otherwise one is taken from torch's allocator on the current stream."""
+    that keep one; otherwise one is taken from torch's allocator."""
     N, D = d_out.shape
     dtype, id_type = _DTYPES.get(d_out.dtype), _ID_TYPES.get(ids.dtype)
     assert dtype is not None and id_type is not None and ids.shape == (N,) and ids.is_contiguous()
     assert out is not None or not accumulate
     if out is None:
-        out = torch.empty((num_rows, D), dtype=torch.float32, device=d_out.device)
+        out = _result((num_rows, D), torch.float32, d_out.device, stream)
     (ldd, one), (ldt, also_one) = d_out.stride(), out.stride()
     to = _DTYPES.get(out.dtype)
     assert to in (dtype, GNNPRE_F32) and out.shape == (num_rows, D) and (D == 1 or one == 1 == also_one)
-    room = _workspace(workspace, _lib.gnnpre_embedding_grad_workspace(num_rows, D, N), "gnnpre_embedding_grad", d_out.device)
+    room = _workspace(workspace, _lib.gnnpre_embedding_grad_workspace(num_rows, D, N), "gnnpre_embedding_grad", d_out.device, stream)
     device = torch.cuda.current_device()
     assert d_out.get_device() == device == ids.get_device() and out.get_device() == device == room.get_device()
     _check(_lib.gnnpre_embedding_grad(d_out.data_ptr(), ldd if N > 1 else max(ldd, D), dtype, ids.data_ptr(), id_type, N, num_rows, D, scale,
                                       int(accumulate), out.data_ptr(), ldt if num_rows > 1 else max(ldt, D), to, room.data_ptr(),
                                       room.numel(), _raw_stream(device) if stream is None else stream.cuda_stream),
            "gnnpre_embedding_grad")
-    if workspace is None and stream is not None:
-        room.record_stream(stream)  # allocated on the current stream, used on another
     return out
 
 
@@ -490,7 +526,7 @@ def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor
         N, bptr = n, None
     else:
         if batch.dtype is torch.int64:
-            batch = _int32_rows(batch, n)
+            batch = _int32_rows(batch, n, stream)
         (N,) = batch.shape
         assert batch.dtype is torch.int32 and batch.is_contiguous() and batch.get_device() == device
         bptr = batch.data_ptr()
@@ -508,25 +544,18 @@ def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor
         layout.append((0, 0))
     assert out is not None or not accumulate
     if out is None:
-        out = torch.empty((H, F), dtype=torch.float32, device=dY.device)
+        out = _result((H, F), torch.float32, dY.device, stream)
     ldw, one = out.stride()
     assert out.dtype is torch.float32 and out.shape == (H, F) and (one == 1 or F == 1) and out.get_device() == device
-    room = _workspace(workspace, _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H), "gnnpre_lc_first_layer_grad", dY.device)
+    room = _workspace(workspace, _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H), "gnnpre_lc_first_layer_grad", dY.device, stream)
     assert room.get_device() == device
-    flag = torch.zeros(1, dtype=torch.int32, device=dY.device) if check else None
-    if check and stream is not None:
-        stream.wait_stream(torch.cuda.current_stream())  # the flag is cleared on the current one
+    flag = _error_word(dY.device, stream) if check else None
     _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, hs[0], bptr, N, dY.data_ptr(), *layout[0],
                                            Y.data_ptr() if Y is not None else None, *layout[1], relu_mask, H, int(accumulate), out.data_ptr(),
                                            ldw, room.data_ptr(), room.numel(), flag.data_ptr() if check else None,
                                            _raw_stream(device) if stream is None else stream.cuda_stream), "gnnpre_lc_first_layer_grad")
-    if workspace is None and stream is not None:
-        room.record_stream(stream)
     if check:
-        if stream is not None:
-            stream.synchronize()
-        if int(flag.item()) != 0:
-            raise GnnpreError(-8, "gnnpre_lc_first_layer_grad")
+        _check_waits(flag, stream, "gnnpre_lc_first_layer_grad")
     return out
 
 
@@ -535,9 +564,9 @@ def gnnpre_lc_grad_selftest_wait_timeout(hop: torch.Tensor, dY: torch.Tensor, po
     n, F = hop.shape
     H = dY.shape[1]
     assert dY.shape[0] == n
-    out = torch.empty((H, F), dtype=torch.float32, device=hop.device)
-    room = torch.empty(gnnpre_lc_first_layer_grad_workspace(1, n, F, H), dtype=torch.uint8, device=hop.device)
-    flag = torch.zeros(1, dtype=torch.int32, device=hop.device)
+    out = _result((H, F), torch.float32, hop.device, stream)
+    room = _workspace(None, gnnpre_lc_first_layer_grad_workspace(1, n, F, H), "gnnpre_lc_grad_selftest_wait_timeout", hop.device, stream)
+    flag = _error_word(hop.device, stream)
     _on_current_device(hop, dY)
     return int(_lib.gnnpre_lc_grad_selftest_wait_timeout(hop.data_ptr(), n, F, hop.stride(0), dY.data_ptr(), dY.stride(0), H,
                                                          out.data_ptr(), F, room.data_ptr(), room.numel(), flag.data_ptr(), polls,
@@ -563,30 +592,23 @@ def gnnpre_orthogonalize(G: torch.Tensor, *, steps: int = 5, coeffs=(3.4445, -4.
     synchronises and raises if a device-side wait ran out."""
     assert G.dim() in (2, 3) and G.dtype in _DTYPES
     if out is None:
-        out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+        out = _result(G.shape, G.dtype, G.device, stream)
     assert out.dtype is G.dtype and out.shape == G.shape
     a, o = (t if t.dim() == 3 else t.unsqueeze(0) for t in (G, out))
     n, rows, cols = a.shape
     assert (a.stride(2) == 1 or cols == 1) and (o.stride(2) == 1 or cols == 1)
     _on_current_device(G, out)
     size = _lib.gnnpre_orthogonalize_workspace(n, rows, cols, steps)
-    room = _workspace(workspace, size, "gnnpre_orthogonalize", G.device)
+    room = _workspace(workspace, size, "gnnpre_orthogonalize", G.device, stream)
     _on_current_device(room)
-    flag = torch.zeros(1, dtype=torch.int32, device=G.device) if check else None
-    if check and stream is not None:
-        stream.wait_stream(torch.cuda.current_stream())  # the flag is cleared on the current one
+    flag = _error_word(G.device, stream) if check else None
     ld = [max(t.stride(1), cols) if rows == 1 else t.stride(1) for t in (a, o)]
     _check(_lib.gnnpre_orthogonalize(a.data_ptr(), rows, cols, ld[0], a.stride(0), n, _DTYPES[G.dtype], steps,
                                      (ctypes.c_float * 3)(*[float(c) for c in coeffs]), eps, scale, o.data_ptr(), ld[1], o.stride(0),
                                      room.data_ptr(), room.numel(), flag.data_ptr() if check else None, _stream_ptr(stream)),
            "gnnpre_orthogonalize")
-    if workspace is None and stream is not None:
-        room.record_stream(stream)
     if check:
-        if stream is not None:
-            stream.synchronize()
-        if int(flag.item()) != 0:
-            raise GnnpreError(-8, "gnnpre_orthogonalize")
+        _check_waits(flag, stream, "gnnpre_orthogonalize")
     return out
 
 
@@ -594,9 +616,9 @@ def gnnpre_orthogonalize_selftest_wait_timeout(G: torch.Tensor, polls: int = 200
     """Status of products whose waits are made to run out (expected: -8, GNNPRE_ERR_TIMEOUT)."""
     rows, cols = G.shape
     assert G.dtype is torch.float32 and G.is_contiguous()
-    out = torch.empty_like(G)
-    room = torch.empty(gnnpre_orthogonalize_workspace(1, rows, cols, 1), dtype=torch.uint8, device=G.device)
-    flag = torch.zeros(1, dtype=torch.int32, device=G.device)
+    out = _result(G.shape, G.dtype, G.device, stream)
+    room = _workspace(None, gnnpre_orthogonalize_workspace(1, rows, cols, 1), "gnnpre_orthogonalize_selftest_wait_timeout", G.device, stream)
+    flag = _error_word(G.device, stream)
     _on_current_device(G)
     return int(_lib.gnnpre_orthogonalize_selftest_wait_timeout(G.data_ptr(), rows, cols, out.data_ptr(), room.data_ptr(), room.numel(),
                                                                flag.data_ptr(), polls, _stream_ptr(stream)))
