@@ -172,7 +172,7 @@ def _result(shape, dtype, device, stream) -> torch.Tensor:
     """A result that the caller did not bring, from the current stream's memory.  If the kernels run on another stream, that one waits for
     the current one, whose work may still use the block, and the allocator is told of the use there."""
     out = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
+    if stream is not None and out.is_cuda:
         _wait_for_current(stream)
         out.record_stream(stream)
     return out
@@ -199,7 +199,7 @@ def _pointers(tensors):
 
 def gnnpre_degrees(rowptr: torch.Tensor, colidx: torch.Tensor, stream=None) -> torch.Tensor:
     csr = _csr(rowptr, colidx)
-    deg = torch.empty(csr.n, dtype=torch.int32, device=rowptr.device)
+    deg = _result((csr.n,), torch.int32, rowptr.device, stream)
     _check(_lib.gnnpre_degrees(ctypes.byref(csr), deg.data_ptr(), _stream_ptr(stream)), "gnnpre_degrees")
     return deg
 
@@ -302,7 +302,7 @@ def gnnpre_propagate(plan: Plan, X: torch.Tensor, K: int, out: Sequence[torch.Te
     if out is None:
         Fp = (F + 3) // 4 * 4  # the library works on whole groups of 4 columns
         if on_device:
-            out = [torch.empty((n, Fp), dtype=torch.float32, device=X.device)[:, :F] for _ in range(K)]
+            out = [_result((n, Fp), torch.float32, X.device, stream)[:, :F] for _ in range(K)]
         else:
             out = [torch.empty((n, Fp), dtype=torch.float32, pin_memory=True)[:, :F] for _ in range(K)]
     assert len(out) == K
@@ -353,10 +353,10 @@ def gnnpre_propagate_weighted(plan: Plan, X: torch.Tensor, gamma, *, out=None, Z
     Fp = (F + 3) // 4 * 4
     if out is None:
         nbuf = K if keep_hops else min(K, 2)
-        bufs = [torch.empty((n, Fp), dtype=torch.float32, device=X.device)[:, :F] for _ in range(nbuf)]
+        bufs = [_result((n, Fp), torch.float32, X.device, stream)[:, :F] for _ in range(nbuf)]
         out = [bufs[k % nbuf] for k in range(K)]
     if Z is None:
-        Z = torch.empty((n, Fp), dtype=torch.float32, device=X.device)[:, :F]
+        Z = _result((n, Fp), torch.float32, X.device, stream)[:, :F]
     for o in list(out) + [Z]:
         assert o.is_cuda and o.dtype == torch.float32 and o.shape == (n, F) and o.stride(1) == 1
     assert all(o.stride(0) == out[0].stride(0) for o in out)
@@ -628,8 +628,7 @@ def gnnpre_normalize(plan: Plan, out: torch.Tensor | None = None, *, host: bool 
     """fp32 value of every edge of the support (order of gnnpre_plan_support), on the device or in host memory."""
     m = plan.nnz_tilde
     if out is None:
-        out = torch.empty(m, dtype=torch.float32, pin_memory=True) if host else torch.empty(
-            m, dtype=torch.float32, device="cuda")
+        out = torch.empty(m, dtype=torch.float32, pin_memory=True) if host else _result((m,), torch.float32, "cuda", stream)
     assert out.dtype == torch.float32 and out.numel() == m and out.is_contiguous()
     _check(_lib.gnnpre_normalize(plan.handle, out.data_ptr(), _mem_of(out), _stream_ptr(stream)), "gnnpre_normalize")
     return out
@@ -666,7 +665,7 @@ def gnnpre_gather_ceiling(plan: Plan, X: torch.Tensor, sink: torch.Tensor | None
     assert X.is_cuda and X.dtype == torch.float32 and X.dim() == 2 and X.stride(1) == 1
     nseg = gnnpre_plan_info(plan)["num_segments"]
     if sink is None:
-        sink = torch.empty(max(nseg, 1), dtype=torch.float32, device=X.device)
+        sink = _result((max(nseg, 1),), torch.float32, X.device, stream)
     assert sink.is_cuda and sink.dtype == torch.float32 and sink.numel() >= nseg and sink.is_contiguous()
     _check(_lib.gnnpre_gather_ceiling(plan.handle, X.data_ptr(), X.stride(0), sink.data_ptr(), _stream_ptr(stream)),
            "gnnpre_gather_ceiling")

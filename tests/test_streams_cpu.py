@@ -103,3 +103,16 @@ def test_on_the_current_stream_nothing_waits(world, name):
     workspace, call, shape = CALLS[name]
     call(B)
     assert not any(e[0] in ("wait", "record") or e[-1] == "side" for e in log)
+
+
+def test_hops_that_a_call_makes_are_ordered_with_its_stream(world):
+    B, side, log = world
+    plan = B.Plan(0, nnz_tilde=7)
+    X = torch.ones((5, 8))
+    for call in (lambda: B.gnnpre_propagate(plan, X, 3, stream=side), lambda: B.gnnpre_propagate_weighted(plan, X, (0.5, 0.5), stream=side),
+                 lambda: B.gnnpre_degrees(torch.zeros(6, dtype=torch.int64), torch.zeros(0, dtype=torch.int32), stream=side)):
+        del log[:]
+        call()
+        log[:] = [e for e in log if e[0] != "zeros"]
+        check_log(log, False)
+        assert ("empty", "current") in log
