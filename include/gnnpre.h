@@ -450,7 +450,7 @@ int gnnpre_embedding_grad(const void* d_out, int64_t ldd, int32_t dtype, const v
  *   error_flag  DEVICE int32 or NULL; set to 1 by the kernel if one of its bounded waits ran out (the results are then invalid).
  *               The caller clears and reads it.
  * hidden a multiple of 16, 16..256; 1 <= feat_dim <= 2^20; 0 <= batch_size < 2^31; strides not negative, ldh, ldw >= feat_dim, lddy,
- * ldy >= hidden; dWt apart from what is read (else INVALID_ARG).  ldh a multiple of 4, hops 16-byte aligned, the other pointers
+ * ldy >= hidden; dWt and the workspace apart from what is read and from each other (else INVALID_ARG).  ldh a multiple of 4, hops 16-byte aligned, the other pointers
  * aligned to their elements (else ALIGN).
  * Arithmetic: operands enter with all 24 bits of fp32 (three bf16 numbers each, the six largest of the nine products), sums in fp32
  * in a fixed order: results are bitwise reproducible on a device.  An operand that is not finite makes the sums it enters NaN.

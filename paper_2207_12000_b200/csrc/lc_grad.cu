@@ -561,14 +561,16 @@ int grad_launch(const float* const* hops, int32_t num_hops, int64_t n, int64_t f
         if (reinterpret_cast<uintptr_t>(hops[k]) % 16) return GNNPRE_ERR_ALIGN;
     }
     const int64_t dw_span = (hidden - 1) * ldw + feat_dim;
-    const auto meets = [&](const void* p, int64_t floats) { return arrays_overlap(dWt, 1, dw_span, 1, 4, p, 1, floats, 1, 4); };
     if (batch_size > 0) {
-        const int64_t rows = (batch_size - 1);
+        const int64_t rows = batch_size - 1, room = grad_shape(num_hops, batch_size, feat_dim, hidden, kMostSms).bytes;
+        if (workspace_bytes < room) return GNNPRE_ERR_INVALID_ARG;
+        // what is written, the sums and the shares' sums before them, lies apart from what is read and from one another
+        const auto meets = [&](const void* p, int64_t floats) {
+            return arrays_overlap(dWt, 1, dw_span, 1, 4, p, 1, floats, 1, 4) || arrays_overlap(workspace, 1, room, 1, 1, p, 1, floats, 1, 4);
+        };
         if (meets(dY, (num_hops - 1) * dy_hop + rows * lddy + hidden) || (used && meets(Y, (num_hops - 1) * y_hop + rows * ldy + hidden)) ||
-            (batch && meets(batch, batch_size)))
+            (batch && meets(batch, batch_size)) || arrays_overlap(dWt, 1, dw_span, 1, 4, workspace, 1, room, 1, 1))
             return GNNPRE_ERR_INVALID_ARG;
-        const int64_t room = grad_shape(num_hops, batch_size, feat_dim, hidden, kMostSms).bytes;
-        if (workspace_bytes < room || meets(workspace, room / 4)) return GNNPRE_ERR_INVALID_ARG;
         for (int32_t k = 0; k < num_hops; ++k)
             if (meets(hops[k], (n - 1) * ldh + feat_dim)) return GNNPRE_ERR_INVALID_ARG;
     }

@@ -137,3 +137,16 @@ def test_lc_grad_workspace(lib):
     for K, rows, F, H in ((1, 1, 1, 16), (3, 4096, 128, 256), (2, 20011, 602, 192), (3, 2449029, 100, 256)):
         tiles = -(-H // 128) * -(-F // 128)
         assert 0 < size(K, rows, F, H) <= 4 * max(1, 192 // tiles) * H * (F + 16 * -(-F // 128))
+
+
+@pytest.mark.parametrize("where", ("dY", "Y", "batch", "hop"))
+def test_lc_grad_refuses_a_workspace_on_its_inputs(lib, where):
+    at = dict(dY=0x4000000, Y=0x4000000 + 0x100, batch=0x4000000 + 0x200)
+    changes = dict(hops=pointers(0x100000, 0x4000000 - 4 * 64 * 999)) if where == "hop" else {where: at[where]}
+    assert call(lib.gnnpre_lc_first_layer_grad, LC_GRAD, **changes) == INVALID_ARG
+
+
+def test_lc_grad_looks_at_no_more_of_its_workspace_than_it_asks_for(lib):
+    """An input behind the part that the call needs is none of its business: the call gets as far as asking for a device."""
+    need = lib.gnnpre_lc_first_layer_grad_workspace(2, 100, 60, 32)
+    assert call(lib.gnnpre_lc_first_layer_grad, LC_GRAD, dY=0x4000000 + need) not in (INVALID_ARG, ALIGN)
