@@ -923,7 +923,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) most = fmaxf(most, largest[w]);
-        const int exponent = most > 0.f && most <= 3.4e38f ? min(max(ilogbf(most), -126), 126) : 0;
+        const int exponent = most > 0.f && isfinite(most) ? min(max(ilogbf(most), -126), 126) : 0;
         const float to_one = ldexpf(1.f, -exponent);
         float sumf = 0.f;
 #pragma unroll

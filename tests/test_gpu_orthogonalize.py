@@ -247,3 +247,16 @@ def test_waits_that_run_out_are_reported_and_leave_the_device_usable(B):
         got = wide(B.gnnpre_orthogonalize(G))
         want = orc.orthogonalize(wide(G), 5, f32(QUINTIC), 1e-7, 1.0)
         assert np.linalg.norm(got - want) <= 2.0 ** -10 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("shape", [(128, 256), (60, 130), (130, 60), (100, 1500), (300, 500), (500, 300), (1500, 1500)])
+def test_the_largest_numbers_are_finite(B, shape):
+    """Entries up to the largest that fp32 holds: the result is that of the same matrix scaled down by a power of two."""
+    G = dense(shape, 4, 1.0)
+    G[3, 5] = -np.abs(G).max() * 2
+    top = np.abs(G).max()
+    G = G / top
+    big = torch.from_numpy((G * np.finfo(np.float32).max).astype(np.float32)).cuda()
+    assert float(big[3, 5]) == -float(np.finfo(np.float32).max)
+    got = B.gnnpre_orthogonalize(big)
+    assert torch.equal(got, B.gnnpre_orthogonalize(big * 2.0 ** -100, eps=0.0)) and float(got.abs().max()) > 0
