@@ -844,8 +844,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
     __shared__ __align__(8) unsigned long long bars[2];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
-    __shared__ double room[kChipThreads / 32], norm;
-    __shared__ float largest[kChipThreads / 32];
+    __shared__ double room[kChipThreads / 32];
     volatile int* abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank, ctas;
@@ -875,9 +874,16 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
 
     {
         // G is read along its rows and laid down as fp32 where X will be: rows of 64 16-byte pieces, turned by the row.  Then every thread
-        // takes 64 columns of a row of X, and once all have theirs, X in two parts takes the place.
+        // takes 64 columns of a row of X, and once all have theirs, X in two parts takes the place.  The squares are added up in 64 bits
+        // between the loads, which hide them (in a pass of its own over the registers: 1.3 us more on [256, 128]).
         constexpr int kWarps = kChipThreads / 32;
         auto place = [&](int i, int j) { return base_p + i * (kChipCols * 4) + (((j >> 2) ^ (i & 31)) << 4) + (j & 3) * 4; };
+        double sum2 = 0, odd2 = 0;
+        auto keep = [&](int i, int j, int k, float v) {
+            *reinterpret_cast<float*>(place(i, j)) = v;
+            double& to = k & 1 ? odd2 : sum2;
+            to = fma((double)v, (double)v, to);
+        };
         auto load = [&](auto* p) {
             p += batch * src.batch_stride;
             if (src.tall) {  // a row of G is a column of X: lanes are rows of X
@@ -887,7 +893,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
                     for (int k = 0; k < 4; ++k) {
                         const int i = 32 * k + lane;
                         const float v = to_f32(p[(int64_t)min(j0 + j, n - 1) * src.ldg + min(i, r - 1)]);
-                        *reinterpret_cast<float*>(place(i, j)) = i < r && j0 + j < n ? v : 0.f;
+                        keep(i, j, k, i < r && j0 + j < n ? v : 0.f);
                     }
             } else {
 #pragma unroll 2
@@ -896,16 +902,20 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
                     for (int k = 0; k < kChipCols / 32; ++k) {
                         const int j = 32 * k + lane;
                         const float v = to_f32(p[(int64_t)min(i, r - 1) * src.ldg + min(j0 + j, n - 1)]);
-                        *reinterpret_cast<float*>(place(i, j)) = i < r && j < a.cols && j0 + j < n ? v : 0.f;
+                        keep(i, j, k, i < r && j < a.cols && j0 + j < n ? v : 0.f);
                     }
             }
         };
         if (src.dtype == GNNPRE_F32) load(static_cast<const float*>(src.g));
         else if (src.dtype == GNNPRE_BF16) load(static_cast<const __nv_bfloat16*>(src.g));
         else load(static_cast<const __half*>(src.g));
+        sum2 += odd2;
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) sum2 += __shfl_xor_sync(0xffffffffu, sum2, d);
+        if (lane == 0) room[warp] = sum2;
         __syncthreads();
         constexpr int kGroups = kChipCols / 32;  // of eight columns
-        float g[kGroups][8], most = 0.f;
+        float g[kGroups][8];
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
             const int c = 8 * (4 * k + piece);
@@ -913,48 +923,21 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             const float4 u = *reinterpret_cast<const float4*>(place(row, c)), w = *reinterpret_cast<const float4*>(place(row, c + 4));
             g[k][0] = u.x, g[k][1] = u.y, g[k][2] = u.z, g[k][3] = u.w;
             g[k][4] = w.x, g[k][5] = w.y, g[k][6] = w.z, g[k][7] = w.w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(g[k][e]));
         }
-        // squares of numbers of size one: neither tiny nor huge updates lose their norm
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        if (lane == 0) largest[warp] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) most = fmaxf(most, largest[w]);
-        const int exponent = most > 0.f && isfinite(most) ? min(max(ilogbf(most), -126), 126) : 0;
-        const float to_one = ldexpf(1.f, -exponent);
-        float sumf = 0.f;
-#pragma unroll
-        for (int k = 0; k < kGroups; ++k)
-            if (8 * (4 * k + piece) < a.cols)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    g[k][e] *= to_one;
-                    sumf = fmaf(g[k][e], g[k][e], sumf);
-                }
-        double sum2 = (double)sumf;
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) sum2 += __shfl_xor_sync(0xffffffffu, sum2, d);
-        if (lane == 0) room[warp] = sum2;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kWarps; ++w) sum2 += room[w];
-            sum2 = ldexp(sum2, 2 * exponent);
-            if (ctas > 1) src.partial[batch * kNormBlocks + rank] = sum2;
-            else norm = sum2;
-        }
+        // the warps' sums and then the CTAs', in their order
+        sum2 = room[0];
+        for (int w = 1; w < kWarps; ++w) sum2 += room[w];
         if (ctas > 1) {
+            if (threadIdx.x == 0) src.partial[batch * kNormBlocks + rank] = sum2;
             ns_cluster_sync();
-            if (threadIdx.x == 0) {
-                sum2 = 0;
-                for (uint32_t c = 0; c < ctas; ++c) sum2 += __ldcg(src.partial + batch * kNormBlocks + c);
-                norm = sum2;
-            }
+            sum2 = 0;
+            for (uint32_t c = 0; c < ctas; ++c) sum2 += __ldcg(src.partial + batch * kNormBlocks + c);
         }
         __syncthreads();
-        const float scale = (float)ldexp(1.0 / (sqrt(norm) + src.eps) * (double)src.factor, exponent);
+        // entries are brought to size one first: neither tiny nor huge ones leave fp32's range
+        const double size = sqrt(sum2);
+        const int exponent = min(max(ilogb(size), -126), 126);
+        const float to_one = ldexpf(1.f, -exponent), scale = (float)ldexp(1.0 / (size + src.eps) * (double)src.factor, exponent);
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
             const int c = 8 * (4 * k + piece);
@@ -962,7 +945,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             float v[8];
             uint4 hi, lo;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = g[k][e] * scale;
+            for (int e = 0; e < 8; ++e) v[e] = g[k][e] * to_one * scale;
             split8(v, hi, lo);
             unsigned char* d = base_p + c / kBlockCols * kBlockBytes + block_byte(row, c % kBlockCols);
             *reinterpret_cast<uint4*>(d) = hi;

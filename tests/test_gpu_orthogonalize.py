@@ -260,3 +260,19 @@ def test_the_largest_numbers_are_finite(B, shape):
     assert float(big[3, 5]) == -float(np.finfo(np.float32).max)
     got = B.gnnpre_orthogonalize(big)
     assert torch.equal(got, B.gnnpre_orthogonalize(big * 2.0 ** -100, eps=0.0)) and float(got.abs().max()) > 0
+
+
+@pytest.mark.parametrize("shape", [(128, 256), (256, 128), (100, 2000), (300, 500), (1500, 1600)])
+def test_the_norm_is_summed_in_64_bits(B, shape):
+    """A few ones along the longer side, before and among entries whose squares, 2^-24 each, fp32 drops beside a one: with them the
+    norm is larger by 2^-19 of itself.  With P = I the result is G / ||G||, off by the operands' rounding (2^-22 for X, its scale and
+    factor 2^-23, the result 2^-24)."""
+    G = np.full(sorted(shape), 2.0 ** -12, dtype=np.float32)
+    for first in (0, 8, 16, 24):
+        G[:, first::256] = 1.0
+    if shape[0] > shape[1]:
+        G = np.ascontiguousarray(G.T)
+    got = wide(B.gnnpre_orthogonalize(torch.from_numpy(G).cuda(), steps=1, coeffs=(1.0, 0.0, 0.0), eps=0.0))
+    want = G.astype(np.float64) / np.sqrt((G.astype(np.float64) ** 2).sum())
+    ones = G == 1.0
+    assert (np.abs(got - want)[ones] <= 2.0 ** -21 * want[ones]).all(), float((np.abs(got - want)[ones] / want[ones]).max() * 2.0 ** 21)
