@@ -493,9 +493,13 @@ int gnnpre_lc_grad_selftest_wait_timeout(const float* hop, int64_t n, int64_t fe
  *               The caller clears and reads it.
  * 1 <= rows, cols <= 65536, 0 <= batch <= 16384, 1 <= steps <= 64, eps >= 0 and finite; ldg, ldo >= cols, matrices of out apart
  * (else INVALID_ARG).  Pointers need the alignment of their elements (else ALIGN).
- * Arithmetic: the norm in fp64; operands of the products carry 22 bits (two fp16 numbers each, scaled by a power of two that the
- * coefficients fix), products summed in fp32, one rounding to the output's type.  A matrix of zeros stays one (with eps = 0 it
- * becomes NaN); a NaN or an infinity anywhere in a matrix makes that matrix NaN.
+ * Arithmetic: the norm in fp64; operands of the products as two fp16 numbers each, scaled by a power of two that the coefficients
+ * and, where ||G|| < eps / 3, the matrix's own norm fix: 22 bits of entries down to some 2^-16 of the largest singular value that an
+ * operand can have, an absolute error of 2^-39 of that value for smaller ones (so a row or column far weaker than its matrix is less
+ * exact in itself than in fp32, though not beside the others).  Norms of X_0 below 2^-90 are held with that much less.  Products summed in
+ * fp32, one rounding to the output's type; 16-bit outputs of matrices that are not square may multiply the polynomials of two (fp16) or
+ * three (bf16) steps together, whose errors lie below that rounding.  A matrix of zeros stays one (with eps = 0 it becomes NaN); a NaN or
+ * an infinity anywhere in a matrix makes that matrix NaN.
  * The work is enqueued on `stream` and the call returns without synchronising; nothing is allocated.
  */
 int64_t gnnpre_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int32_t steps);

@@ -7,8 +7,10 @@
 // Numbers.  ||X_0||_F <= 1, so every singular value starts in [0, 1] and the polynomial's coefficients bound all that follows
 // (computed on the host; coefficients under which the iterates may grow without such a bound are refused).  A matrix with a known
 // bound is held as 2^e times itself in two fp16 numbers, high and low part, e chosen so that the bound just fits: 22 significant
-// bits, and an absolute error far below that of fp32 sums of the same size.  A product takes three tensor-core products (high x
-// high, high x low, low x high) into one fp32 accumulator; what is dropped is below 2^-22 of the operands.  fp16 carries
+// bits of entries down to some 2^-16 of the bound, and of smaller ones an absolute error of 2^-39 of it, far below that of fp32 sums of
+// that size.  (An update whose norm is far below eps starts far below one: the device finds bounds for it from its norm.)  A product
+// takes three tensor-core products (high x high, high x low, low x high) into one fp32 accumulator; what is dropped is below 2^-22 of
+// the operands.  fp16 carries
 // 11 bits where tf32 carries as many at half the rate and bf16 carries 8: one fp16 product in place of the three would lose the
 // small singular values, which a step multiplies by a (3.4) and with them the rounding errors of the large ones.
 //
@@ -79,6 +81,62 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo
     lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
+// ------------------------------------------------------------------------------------------------ exponents
+
+struct Coeffs {
+    float a, b, c;
+};
+
+constexpr double kLeastSpectral = 0x1p-90;  // what lies below is held as if it were as large (its squares leave fp32 at 2^-63)
+constexpr double kOwnBounds = 0.25;         // norms of X_0 from here on cost at most two of the 22 bits: the coefficients' bounds do
+
+// 2^e with which a matrix of this bound fits fp16 with room to spare.
+__host__ __device__ inline int exponent_for(double bound) { return 14 - ilogb(fmax(bound, 1e-200)); }
+
+// Of c A + b I, A's second form, where X has this bound.
+__host__ __device__ inline int second_exponent(const Coeffs& c, double x) { return exponent_for(fabs((double)c.c) * x * x + fabs((double)c.b)); }
+
+// Bounds of |P| and of the next X where X's bound x is its own and lies below the one that the coefficients give, which says `all_p` and
+// `all_next`.
+__device__ inline void own_bounds(const Coeffs& c, double x, double all_p, double all_next, double* p, double* next) {
+    const double t = x * x;
+    *p = fmin(all_p, fabs((double)c.a) + (fabs((double)c.b) + fabs((double)c.c) * t) * t);
+    *next = fmax(fmin(all_next, x * *p * (1.0 + 1e-4)), kLeastSpectral);
+}
+
+// Bound of an X_0 of this norm.
+__device__ inline double first_bound(double norm_of_x) { return fmax(norm_of_x * (1.0 + 1e-4), kLeastSpectral); }
+
+// What the products of a step are multiplied by, between the exponents of what goes in and of what comes out.
+struct StepFactors {
+    float gram;           // A = X X^T
+    float gram2, diag2;   // its second form (k_ns_chip: of c A A and b A in P)
+    float p, p_diag;      // P
+    float apply;          // X = P X
+    float out;            // the caller's matrix = P X
+};
+
+// `ex`: X's exponent, and then the next X's.
+__host__ __device__ inline StepFactors step_factors(const Coeffs& c, bool chip, float scale, double x, double p, double next, int* ex) {
+    const int ea = exponent_for(x * x), ep = exponent_for(p), e2 = chip ? ep : second_exponent(c, x), en = exponent_for(next);
+    StepFactors f;
+    f.gram = (float)ldexp(1.0, ea - 2 * *ex);
+    f.gram2 = (float)ldexp((double)c.c, chip ? ep - 2 * ea : e2 - 2 * *ex);
+    f.diag2 = (float)ldexp((double)c.b, chip ? ep - ea : e2);
+    f.p = (float)ldexp(1.0, ep - ea - e2);
+    f.p_diag = (float)ldexp((double)c.a, ep);
+    f.apply = (float)ldexp(1.0, en - ep - *ex);
+    f.out = (float)ldexp((double)scale, -ep - *ex);
+    *ex = en;
+    return f;
+}
+
+// The coefficients' bounds: of X before a step, of |P| in it.
+struct AllBounds {
+    Coeffs c;
+    double x[kMaxSteps + 1], p[kMaxSteps];
+};
+
 // ------------------------------------------------------------------------------------------------ norm and first split
 
 struct Source {
@@ -133,8 +191,40 @@ __global__ void __launch_bounds__(kNormThreads) k_ns_norm(const Source s) {
     }
 }
 
+// Of a launch per product: how much larger than the coefficients' exponents a matrix's own ones are, for each kind of operand and step.
+enum { kOfX, kOfA, kOfA2, kOfP, kOfQ, kOfT, kKinds };
+constexpr int kSlots = kKinds * (kMaxSteps + 1);
+__host__ __device__ inline int slot(int kind, int step) { return kind * (kMaxSteps + 1) + step; }
+
+struct Own {
+    AllBounds all;
+    int32_t steps, segment;  // (Q is the product of the P of a segment so far)
+    int32_t* by;             // [batch][kSlots]
+};
+
+// One thread's work; small: X_0's norm lies below kOwnBounds.
+__device__ inline void own_exponents(const Own& o, double norm_of_x, int32_t* by) {
+    double x = first_bound(norm_of_x), all_q = 1, q = 1;
+    for (int k = 0; k <= o.steps; ++k) {
+        const double all_x = o.all.x[k];
+        by[slot(kOfX, k)] = exponent_for(x) - exponent_for(all_x);
+        if (k == o.steps) break;
+        const double all_p = o.all.p[k];
+        double p, next;
+        own_bounds(o.all.c, x, all_p, o.all.x[k + 1], &p, &next);
+        all_q = k % o.segment ? all_q * all_p : all_p;
+        q = k % o.segment ? q * p : p;
+        by[slot(kOfA, k)] = exponent_for(x * x) - exponent_for(all_x * all_x);
+        by[slot(kOfA2, k)] = second_exponent(o.all.c, x) - second_exponent(o.all.c, all_x);
+        by[slot(kOfP, k)] = exponent_for(p) - exponent_for(all_p);
+        by[slot(kOfQ, k)] = exponent_for(q) - exponent_for(all_q);
+        by[slot(kOfT, k)] = exponent_for(x * x * p) - exponent_for(all_x * all_x * all_p);
+        x = next;
+    }
+}
+
 // X and its transpose, split: a CTA takes [64, 64] of X.
-__global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t norm_blocks) {
+__global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t norm_blocks, const __grid_constant__ Own own) {
     __shared__ float tile[64][65];
     __shared__ double inverse;
     const int64_t batch = blockIdx.z;
@@ -152,10 +242,20 @@ __global__ void __launch_bounds__(256) k_ns_split(const Source s, const int32_t 
         for (int b = threadIdx.x; b < norm_blocks; b += 32) sum += s.partial[batch * kNormBlocks + b];
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (threadIdx.x == 0) inverse = 1.0 / (sqrt(sum) + s.eps);
+        const double norm = sqrt(sum), over = 1.0 / (norm + s.eps), norm_of_x = norm * over;
+        const bool small = norm_of_x < kOwnBounds;
+        if (threadIdx.x == 0) inverse = over * (small ? ldexp(1.0, exponent_for(first_bound(norm_of_x))) : (double)s.factor);
+        if (blockIdx.x == 0 && blockIdx.y == 0) {
+            int32_t* by = own.by + batch * kSlots;
+            if (!small) {
+                for (int i = threadIdx.x; i < kSlots; i += 32) by[i] = 0;
+            } else if (threadIdx.x == 0) {
+                own_exponents(own, norm_of_x, by);
+            }
+        }
     }
     __syncthreads();
-    const double scale = inverse * (double)s.factor;
+    const double scale = inverse;
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
         const int slow = (threadIdx.x >> 6) + 4 * u;
@@ -192,11 +292,13 @@ struct Job {
     float alpha, diag, alpha2, diag2;
     int32_t k_chunks;
     int32_t write_t, write_2;  // write_t: D's transpose as well
+    int32_t of_a, of_b, of_d, of_d2;  // whose exponents they have: slots of `by`
 };
 
 struct Product {
     Job job[2];
     int32_t jobs;
+    const int32_t* by;   // a matrix's own exponents
     int32_t tiles_n;     // of BN columns
     int32_t symmetric;   // D = D^T: only tiles on and below the diagonal, the others by their transposes
     int32_t* error;
@@ -228,6 +330,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
     __shared__ __align__(8) unsigned long long bars[2 * kStages + 2 * kTurns + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
+    __shared__ float alphas[2], diags[2], out_factor;  // of D's forms, with the matrices' own exponents
     volatile int* abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (tc_smem(ns_smem) + 1023u) & ~1023u;
@@ -274,6 +377,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
     float sum[kCols];
     bool ok = true;
     if (warp < kSumWarps) {
+        if (threadIdx.x == 0) {  // (read after the products)
+            const int32_t* by = a.by + batch * kSlots;
+            const int in = by[job.of_a] + by[job.of_b], d = by[job.of_d], d2 = by[job.of_d2];
+            alphas[0] = ldexpf(job.alpha, d - in);
+            alphas[1] = ldexpf(job.alpha2, d2 - in);
+            diags[0] = ldexpf(job.diag, d);
+            diags[1] = ldexpf(job.diag2, d2);
+            out_factor = ldexpf(a.out_factor, -in);
+        }
 #pragma unroll
         for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
         const uint32_t taddr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (warp >> 2) * kCols;
@@ -375,11 +487,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
     const int q = warp & 3, half = (warp >> 2) & 1, row = 32 * q + lane;
     if (ok && a.out) {
         float* line = reinterpret_cast<float*>(base_p) + warp * (32 * 33);
+        const float factor = out_factor;
         if (warp < kSumWarps)
 #pragma unroll
             for (int part = 0; part < kCols / 32; ++part) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[32 * part + j] * a.out_factor;
+                for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[32 * part + j] * factor;
                 __syncwarp();
                 const int col = bj * BN + half * kCols + 32 * part + lane;
                 if (col < a.out_cols)
@@ -407,7 +520,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
             const int form = kApart && transposed ? pass / 2 : pass;
             const bool plain = !kApart || !transposed || pass % 2 == 0, turned = transposed && (!kApart || pass % 2 == 1);
             const Split& to = form ? job.d2 : job.d;
-            const float alpha = form ? job.alpha2 : job.alpha, on_diag = form ? job.diag2 : job.diag;
+            const float alpha = alphas[form], on_diag = diags[form];
             if (pass) __syncthreads();  // (the pass before's copies have read their tiles: thread 0 has waited)
             if (warp < kSumWarps)
 #pragma unroll
@@ -480,10 +593,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_product(const __grid_
 // for one another between products (three per step).  A product by itself takes some 7.5 us as a launch of its own: its CTAs
 // start, set up barriers and tensor memory, wait for the first copies, and leave.
 struct Steps {
-    float gram[kMaxSteps];                        // alpha of A = X X^T
-    float gram2[kMaxSteps], diag2[kMaxSteps];     // alpha and diag of its second form (one launch: of c A A and b A in P)
-    float p[kMaxSteps], p_diag[kMaxSteps];        // alpha and diag of P
-    float apply[kMaxSteps];                       // alpha of X = P X
+    StepFactors by_all[kMaxSteps];  // with the coefficients' bounds
+    AllBounds all;
+    float scale;
 };
 
 struct Cluster {
@@ -492,7 +604,6 @@ struct Cluster {
     int32_t rp, np, k_r, k_n, steps;
     void* out;
     int64_t ldo, out_batch;
-    float out_factor;
     int32_t* error;
     uint32_t spin_limit;
     int32_t drop;
@@ -593,10 +704,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     if (threadIdx.x < 32) {  // the CTAs' sums, in their order
         double v = lane < (int)ctas ? __ldcg(src.partial + batch * kNormBlocks + lane) : 0.0, total = 0;
         for (int c = 0; c < (int)ctas; ++c) total += __shfl_sync(0xffffffffu, v, c);
-        if (lane == 0) room[0] = 1.0 / (sqrt(total) + src.eps) * (double)src.factor;
+        if (lane == 0) {
+            room[0] = 1.0 / (sqrt(total) + src.eps);
+            room[1] = sqrt(total) * room[0];
+        }
     }
     __syncthreads();
-    const double scale = room[0];
+    const double norm_of_x = room[1];
+    const bool small = norm_of_x < kOwnBounds;
+    double bound = first_bound(norm_of_x);  // of X, where it goes by its own; and X's exponent
+    int ex = exponent_for(bound);
+    const double scale = room[0] * (small ? ldexp(1.0, ex) : (double)src.factor);
+    StepFactors f;
     for (int t = rank, k = 0; t < tiles; t += ctas, ++k) {
         const int i0 = t / side_tiles * 64, j0 = t % side_tiles * 64;
         for (int c = threadIdx.x; c < 64 * 8; c += kProductThreads) {
@@ -629,6 +748,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
     for (int stage = 0; stage < 3 * a.steps; ++stage) {
         const int step = stage / 3, kind = stage % 3;
         const bool last = stage == 3 * a.steps - 1, tall = last && src.tall;
+        if (kind == 0) {
+            f = a.s.by_all[step];
+            if (small) {
+                double p, next;
+                own_bounds(a.s.all.c, bound, a.s.all.p[step], a.s.all.x[step + 1], &p, &next);
+                f = step_factors(a.s.all.c, false, a.s.scale, bound, p, next, &ex);
+                bound = next;
+            }
+        }
         const Split& xt = a.xt[step & 1];
         const Split& sa = kind == 0 ? src.x : kind == 1 ? a.a : tall ? xt : a.p;
         const Split& sb = kind == 0 ? src.x : kind == 1 ? a.a2 : tall ? a.p : xt;
@@ -658,7 +786,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
                     if (!ok) continue;
                     float* line = reinterpret_cast<float*>(staging_p) + warp * (32 * 33);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[j] * a.out_factor;
+                    for (int j = 0; j < 32; ++j) line[lane * 33 + j] = sum[j] * f.out;
                     __syncwarp();
                     const int col = bj * BN + half * kCols + lane;
                     if (col < src.cols)
@@ -705,12 +833,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_ns_cluster(const __grid_
                     }
                 };
                 if (kind == 0) {
-                    stage_tile(staging_p, a.s.gram[step], 0.f, false);
-                    stage_tile(staging_p + kBlockBytes, a.s.gram2[step], a.s.diag2[step], false);
+                    stage_tile(staging_p, f.gram, 0.f, false);
+                    stage_tile(staging_p + kBlockBytes, f.gram2, f.diag2, false);
                 } else if (kind == 1) {
-                    stage_tile(staging_p, a.s.p[step], a.s.p_diag[step], false);
+                    stage_tile(staging_p, f.p, f.p_diag, false);
                 } else {
-                    stage_tile(staging_p, a.s.apply[step], 0.f, true);
+                    stage_tile(staging_p, f.apply, 0.f, true);
                 }
                 tc_fence_async();
                 ns_sum_warps_sync();
@@ -820,7 +948,6 @@ struct Chip {
     int32_t steps;
     void* out;
     int64_t ldo, out_batch;
-    float out_factor;
     int32_t* error;
     uint32_t spin_limit;
     int32_t drop;
@@ -845,6 +972,9 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
     __shared__ double room[kChipThreads / 32];
+    __shared__ StepFactors f;  // of a step
+    __shared__ double bound;   // of X where it goes by its own, else 0; and X's exponent (one thread keeps them and f)
+    __shared__ int ex;
     volatile int* abort_flag = &abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank, ctas;
@@ -935,9 +1065,16 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
         }
         __syncthreads();
         // entries are brought to size one first: neither tiny nor huge ones leave fp32's range
-        const double size = sqrt(sum2);
+        const double size = sqrt(sum2), over = 1.0 / (size + src.eps), norm_of_x = size * over;
+        const bool small = norm_of_x < kOwnBounds;
+        const double first = small ? first_bound(norm_of_x) : 0.0;
+        const float to_fp16 = small ? ldexpf(1.f, exponent_for(first)) : src.factor;
+        if (threadIdx.x == kChipThreads - 32) {
+            bound = first;
+            ex = exponent_for(first);
+        }
         const int exponent = min(max(ilogb(size), -126), 126);
-        const float to_one = ldexpf(1.f, -exponent), scale = (float)ldexp(1.0 / (size + src.eps) * (double)src.factor, exponent);
+        const float to_one = ldexpf(1.f, -exponent), scale = (float)ldexp(over * (double)to_fp16, exponent);
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
             const int c = 8 * (4 * k + piece);
@@ -1029,10 +1166,21 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
                 for (int j = 0; j < kBlockCols / 16; ++j) tc_mma(tmem + 128 * b, h + 2 * j, h + 2 * j, square, b == 0 || j != 0);
             }
         }
+        if (threadIdx.x == kChipThreads - 32) {  // (everybody has done with the last step's, and nobody reads these before finish)
+            if (bound > 0.0) {
+                double p, next;
+                own_bounds(a.s.all.c, bound, a.s.all.p[step], a.s.all.x[step + 1], &p, &next);
+                f = step_factors(a.s.all.c, true, a.s.scale, bound, p, next, &ex);
+                bound = next;
+            } else {
+                f = a.s.by_all[step];
+            }
+        }
+        __syncwarp();
         finish();
         float av[32];
         read32(32 * piece, blocks, 128, av);
-        times(av, a.s.gram[step]);
+        times(av, f.gram);
         if (ctas > 1) {
             // The shares' sums, laid down where A will be: rows of 32 pieces of 16 bytes, turned by the row.  Half of the rows at a time
             // the CTAs' are read piece by piece as they lie, neighbouring lanes neighbouring pieces (a lane to a row: 40 us a step
@@ -1095,8 +1243,8 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             const int col = 32 * piece;
             float o[32];
             read32(col, 2, 128, o);
-            times(o, a.s.gram2[step]);
-            const float2 b = make_float2(a.s.diag2[step], a.s.diag2[step]);
+            times(o, f.gram2);
+            const float2 b = make_float2(f.diag2, f.diag2);
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
                 const float2 two = __ffma2_rn(b, make_float2(av[j], av[j + 1]), make_float2(o[j], o[j + 1]));
@@ -1106,7 +1254,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             if (piece == q) {  // the diagonal's warps
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (j == lane) o[j] += a.s.p_diag[step];
+                    if (j == lane) o[j] += f.p_diag;
             }
             write32(as_p, col, o);
         }
@@ -1136,7 +1284,7 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             float o[32];
             read32(col, 2, 256, o);
             if (!last) {
-                times(o, a.s.apply[step]);
+                times(o, f.apply);
                 write32(base_p, col, o);
                 continue;
             }
@@ -1150,11 +1298,11 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
             if (src.tall) {  // neighbouring lanes are neighbours in out's rows
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (row < r && j0 + col + j < n) store(j0 + col + j, row, o[j] * a.out_factor);
+                    if (row < r && j0 + col + j < n) store(j0 + col + j, row, o[j] * f.out);
             } else {
                 float* line = reinterpret_cast<float*>(as_p) + warp * (32 * 32);  // (P has been read); columns turned by the row
 #pragma unroll
-                for (int j = 0; j < 32; ++j) line[lane * 32 + (j ^ lane)] = o[j] * a.out_factor;
+                for (int j = 0; j < 32; ++j) line[lane * 32 + (j ^ lane)] = o[j] * f.out;
                 __syncwarp();
                 if (j0 + col + lane < n)
                     for (int i = 0; i < 32 && 32 * q + i < r; ++i) store(32 * q + i, j0 + col + lane, line[i * 32 + (lane ^ i)]);
@@ -1179,18 +1327,14 @@ __global__ void __launch_bounds__(kChipThreads, 1) k_ns_chip(const __grid_consta
 
 // ------------------------------------------------------------------------------------------------ host
 
-struct Bounds {
-    double x[kMaxSteps + 1];  // largest singular value before step k
-    double p[kMaxSteps];      // largest eigenvalue of |P| in step k
-};
-
 // How large the polynomials can make the singular values, which start in [0, 1]; false: beyond kMostSpectral.
-bool bounds_of(const float* coeffs, int32_t steps, Bounds* out) {
+bool bounds_of(const float* coeffs, int32_t steps, AllBounds* out) {
     const double a = coeffs[0], b = coeffs[1], c = coeffs[2];
+    out->c = Coeffs{coeffs[0], coeffs[1], coeffs[2]};
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
     double r = 1.0;
     for (int32_t k = 0; k < steps; ++k) {
-        r *= 1.0 + 1e-4;  // what rounding adds
+        r = std::max(r * (1.0 + 1e-4), kLeastSpectral);  // (what rounding adds)
         out->x[k] = r;
         const double u1 = r * r;
         const auto p = [&](double u) { return std::fabs(a + b * u + c * u * u); };
@@ -1216,15 +1360,9 @@ bool bounds_of(const float* coeffs, int32_t steps, Bounds* out) {
         r = mx;
         if (!(r <= kMostSpectral) || !(mp <= 1024.0)) return false;
     }
-    out->x[steps] = r;
+    out->x[steps] = std::max(r, kLeastSpectral);
     return true;
 }
-
-// 2^e with which a matrix of this bound fits fp16 with room to spare.
-int exponent_for(double bound) { return std::max(-8, std::min(14, (int)std::floor(std::log2(32768.0 / std::max(bound, 1e-6))))); }
-
-// Of c A + b I, A's second form, where X has this bound.
-int second_exponent(const float* coeffs, double x) { return exponent_for(std::fabs(coeffs[2]) * x * x + std::fabs(coeffs[1])); }
 
 struct NsShape {
     int64_t r, n, rp, np, batch;
@@ -1232,7 +1370,7 @@ struct NsShape {
     int32_t ctas;     // of the cluster that does all of a matrix; 0: a launch per product
     bool chip;        // ... from shared memory
     int64_t side, square;  // bytes of one split [rp, np], [rp, rp]
-    int64_t xt[2], x, a, a2, t, p, q[2], partial, total;
+    int64_t xt[2], x, a, a2, t, p, q[2], partial, by, total;
 };
 
 // Steps of a segment at most (see above).
@@ -1280,6 +1418,7 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     s.q[1] = s.segment > 1 ? take(s.square) : s.p;
     s.t = s.segment > 1 ? take(s.square) : s.p;
     s.partial = take((int64_t)sizeof(double) * kNormBlocks);
+    if (!s.ctas) s.by = take((int64_t)sizeof(int32_t) * kSlots);
     s.total = at;
     return s;
 }
@@ -1362,8 +1501,9 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
               int64_t workspace_bytes, int32_t* error_flag, void* stream, const NsSelfTest* test = nullptr) {
     if (!is_dtype(dtype) || rows < 1 || cols < 1 || rows > kMaxSide || cols > kMaxSide || batch < 0 || batch > 16384) return GNNPRE_ERR_INVALID_ARG;
     if (steps < 1 || steps > kMaxSteps || !coeffs || !(eps >= 0.f) || !std::isfinite(eps)) return GNNPRE_ERR_INVALID_ARG;
-    Bounds bound;
-    if (!bounds_of(coeffs, steps, &bound)) return GNNPRE_ERR_INVALID_ARG;
+    Own own{};
+    AllBounds& all = own.all;
+    if (!bounds_of(coeffs, steps, &all)) return GNNPRE_ERR_INVALID_ARG;
     if (batch == 0) return GNNPRE_OK;
     if (!G || !out || !workspace || ldg < cols || ldo < cols) return GNNPRE_ERR_INVALID_ARG;
     if (batch > 1 && (g_stride < 0 || o_stride < (rows - 1) * ldo + cols)) return GNNPRE_ERR_INVALID_ARG;
@@ -1384,27 +1524,18 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
     const auto side_t = [&](int64_t at) { return Split{w + at, s.side, (int32_t)(s.rp / 64)}; };
     const auto square = [&](int64_t at) { return Split{w + at, s.square, (int32_t)(s.rp / 64)}; };
 
-    int ex = exponent_for(bound.x[0]);
+    int ex = exponent_for(all.x[0]);
     Source src{G, ldg, g_stride, (int32_t)rows, (int32_t)cols, dtype, rows > cols, (double)eps, reinterpret_cast<double*>(w + s.partial),
                (float)std::ldexp(1.0, ex), side(s.x), side_t(s.xt[0])};
     Steps factors{};
-    float out_factor = 0.f;
+    factors.all = all;
+    factors.scale = scale;
     if (s.ctas)
-        for (int32_t k = 0; k < steps; ++k) {
-            const int ea = exponent_for(bound.x[k] * bound.x[k]), ep = exponent_for(bound.p[k]), ex_new = exponent_for(bound.x[k + 1]);
-            const int e2 = s.chip ? ep : second_exponent(coeffs, bound.x[k]);
-            factors.gram[k] = (float)std::ldexp(1.0, ea - 2 * ex);
-            factors.gram2[k] = (float)std::ldexp((double)coeffs[2], s.chip ? ep - 2 * ea : e2 - 2 * ex);
-            factors.diag2[k] = (float)std::ldexp((double)coeffs[1], s.chip ? ep - ea : e2);
-            factors.p[k] = (float)std::ldexp(1.0, ep - ea - e2);
-            factors.p_diag[k] = (float)std::ldexp((double)coeffs[0], ep);
-            factors.apply[k] = (float)std::ldexp(1.0, ex_new - ep - ex);
-            out_factor = (float)std::ldexp((double)scale, -ep - ex);  // of the last step
-            ex = ex_new;
-        }
+        for (int32_t k = 0; k < steps; ++k)
+            factors.by_all[k] = step_factors(all.c, s.chip, scale, all.x[k], all.p[k], all.x[k + 1], &ex);
     if (s.chip) {
         const int64_t cols = ((s.n + s.ctas - 1) / s.ctas + 63) / 64 * 64;
-        const Chip c{src, (int32_t)cols, steps, out, ldo, o_stride, out_factor, error_flag, test ? test->polls : kTcSpinLimit, test ? test->drop : 0, factors};
+        const Chip c{src, (int32_t)cols, steps, out, ldo, o_stride, error_flag, test ? test->polls : kTcSpinLimit, test ? test->drop : 0, factors};
         return launch_clusters(k_ns_chip, kChipThreads, kChipSmem, s.ctas, batch, st, c);
     }
     if (s.ctas) {
@@ -1426,75 +1557,86 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
         c.error = error_flag;
         c.spin_limit = test ? test->polls : kTcSpinLimit;
         c.drop = test ? test->drop : 0;
-        c.out_factor = out_factor;
         c.s = factors;
         return launch_clusters(k_ns_cluster, kProductThreads, kClusterSmem, s.ctas, batch, st, c);
     }
+    own.steps = steps;
+    own.segment = s.segment;
+    own.by = reinterpret_cast<int32_t*>(w + s.by);
     const int norm_blocks = (int)std::min<int64_t>(kNormBlocks, rows);
     k_ns_norm<<<dim3((unsigned)norm_blocks, (unsigned)batch), kNormThreads, 0, st>>>(src);
     GNNPRE_CUDA(cudaGetLastError());
-    GNNPRE_TRY(launch_after(k_ns_split, dim3((unsigned)(s.np / 64), (unsigned)(s.rp / 64), (unsigned)batch), 256, 0, true, st, src, norm_blocks));
+    GNNPRE_TRY(launch_after(k_ns_split, dim3((unsigned)(s.np / 64), (unsigned)(s.rp / 64), (unsigned)batch), 256, 0, true, st, src, norm_blocks, own));
 
     Product base{};
     base.error = error_flag;
     base.spin_limit = test ? test->polls : kTcSpinLimit;
     base.drop = test ? test->drop : 0;
     base.jobs = 1;
+    base.by = own.by;
     const int32_t k_r = (int32_t)((s.r + 63) / 64), k_n = (int32_t)((s.n + 63) / 64);
     int xt = 0;
     for (int32_t k = 0; k < steps;) {
         const int32_t g = std::min(s.segment, steps - k);
-        int ea = exponent_for(bound.x[k] * bound.x[k]), e2 = second_exponent(coeffs, bound.x[k]);
+        int ea = exponent_for(all.x[k] * all.x[k]), e2 = second_exponent(all.c, all.x[k]);
         // a new A from an accumulator that holds 2^acc of it
-        const auto new_a = [&](Job& job, int acc) {
+        const auto new_a = [&](Job& job, int32_t step, int acc) {
             job.d = square(s.a);
+            job.of_d = slot(kOfA, step);
+            job.of_d2 = slot(kOfA2, step);
             job.alpha = (float)std::ldexp(1.0, ea - acc);
             job.d2 = square(s.a2);
             job.alpha2 = (float)std::ldexp((double)coeffs[2], e2 - acc);
             job.diag2 = (float)std::ldexp((double)coeffs[1], e2);
             job.write_2 = 1;
         };
-        const auto operands = [](const Split& x, const Split& y, int32_t chunks) {
+        const auto operands = [](const Split& x, int of_x, const Split& y, int of_y, int32_t chunks) {
             Job job{};
             job.a = x;
             job.b = y;
+            job.of_a = of_x;
+            job.of_b = of_y;
             job.k_chunks = chunks;
             return job;
         };
         Product m = base;
-        m.job[0] = operands(side(s.x), side(s.x), k_n);
-        new_a(m.job[0], 2 * ex);
+        m.job[0] = operands(side(s.x), slot(kOfX, k), side(s.x), slot(kOfX, k), k_n);
+        new_a(m.job[0], k, 2 * ex);
         GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
         int eq = 0, q = 0;
         double q_bound = 1;
         for (int32_t j = 0; j < g; ++j) {
             // P = a I + A (c A + b I)
-            const int ep = exponent_for(bound.p[k + j]);
+            const int ep = exponent_for(all.p[k + j]);
             const Split p = square(j == 0 ? s.q[0] : s.p);
             m = base;
-            m.job[0] = operands(square(s.a), square(s.a2), k_r);
+            const int of_p = slot(kOfP, k + j);
+            m.job[0] = operands(square(s.a), slot(kOfA, k + j), square(s.a2), slot(kOfA2, k + j), k_r);
             m.job[0].d = p;
+            m.job[0].of_d = of_p;
             m.job[0].alpha = (float)std::ldexp(1.0, ep - ea - e2);
             m.job[0].diag = (float)std::ldexp((double)coeffs[0], ep);
             GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
-            q_bound *= bound.p[k + j];
+            q_bound *= all.p[k + j];
             const int eq_new = j == 0 ? ep : exponent_for(q_bound);
-            Job more = operands(square(s.q[q]), p, k_r);
+            Job more = operands(square(s.q[q]), slot(kOfQ, k + j - 1), p, of_p, k_r);  // (from the second step on)
             more.d = square(s.q[q ^ 1]);
+            more.of_d = slot(kOfQ, k + j);
             more.alpha = (float)std::ldexp(1.0, eq_new - eq - ep);
             m = base;
             if (j + 1 < g) {
                 // T = A P, then the next A = T P beside Q = Q P
-                const int et = exponent_for(bound.x[k + j] * bound.x[k + j] * bound.p[k + j]);
-                m.job[0] = operands(square(s.a), p, k_r);
+                const int et = exponent_for(all.x[k + j] * all.x[k + j] * all.p[k + j]);
+                m.job[0] = operands(square(s.a), slot(kOfA, k + j), p, of_p, k_r);
                 m.job[0].d = square(s.t);
+                m.job[0].of_d = slot(kOfT, k + j);
                 m.job[0].alpha = (float)std::ldexp(1.0, et - ea - ep);
                 GNNPRE_TRY(launch_product(m, s.rp, s.rp, batch, true, sms, st));
-                ea = exponent_for(bound.x[k + j + 1] * bound.x[k + j + 1]);
-                e2 = second_exponent(coeffs, bound.x[k + j + 1]);
+                ea = exponent_for(all.x[k + j + 1] * all.x[k + j + 1]);
+                e2 = second_exponent(all.c, all.x[k + j + 1]);
                 m = base;
-                m.job[0] = operands(square(s.t), p, k_r);
-                new_a(m.job[0], et + ep);
+                m.job[0] = operands(square(s.t), slot(kOfT, k + j), p, of_p, k_r);
+                new_a(m.job[0], k + j + 1, et + ep);
                 if (j > 0) {
                     m.job[1] = more;
                     m.jobs = 2;
@@ -1507,12 +1649,14 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
             if (j > 0) q ^= 1;
             eq = eq_new;
         }
+        const int of_q = slot(kOfQ, k + g - 1), of_x = slot(kOfX, k);
         k += g;
         m = base;
         if (k < steps) {
-            const int ex_new = exponent_for(bound.x[k]);
-            m.job[0] = operands(square(s.q[q]), side_t(s.xt[xt]), k_r);
+            const int ex_new = exponent_for(all.x[k]);
+            m.job[0] = operands(square(s.q[q]), of_q, side_t(s.xt[xt]), of_x, k_r);
             m.job[0].d = side(s.x);
+            m.job[0].of_d = slot(kOfX, k);
             m.job[0].dt = side_t(s.xt[xt ^ 1]);
             m.job[0].write_t = 1;
             m.job[0].alpha = (float)std::ldexp(1.0, ex_new - eq - ex);
@@ -1530,7 +1674,7 @@ int ns_launch(const void* G, int64_t rows, int64_t cols, int64_t ldg, int64_t g_
         m.out_factor = (float)std::ldexp((double)scale, -eq - ex);
         // Q is symmetric: the transpose of Q X is X^T Q
         const bool tall = rows > cols;
-        m.job[0] = operands(tall ? side_t(s.xt[xt]) : square(s.q[q]), tall ? square(s.q[q]) : side_t(s.xt[xt]), k_r);
+        m.job[0] = tall ? operands(side_t(s.xt[xt]), of_x, square(s.q[q]), of_q, k_r) : operands(square(s.q[q]), of_q, side_t(s.xt[xt]), of_x, k_r);
         GNNPRE_TRY(launch_product(m, tall ? s.np : s.rp, tall ? s.rp : s.np, batch, false, sms, st));
     }
     return GNNPRE_OK;

@@ -276,3 +276,69 @@ def test_the_norm_is_summed_in_64_bits(B, shape):
     want = G.astype(np.float64) / np.sqrt((G.astype(np.float64) ** 2).sum())
     ones = G == 1.0
     assert (np.abs(got - want)[ones] <= 2.0 ** -21 * want[ones]).all(), float((np.abs(got - want)[ones] / want[ones]).max() * 2.0 ** 21)
+
+
+SMALL = [(128, 256), (256, 100), (60, 1500), (300, 500), (500, 300), (1500, 1600), (1600, 1500)]
+
+
+def near(got, G, steps, coeffs, eps, scale, dtype, carried=0.0):
+    """Whether `got` is as near the oracle as plain fp32 is (eight times its error, as in test_dense), and rounded once."""
+    want = orc.orthogonalize(wide(G), steps, f32(coeffs), float(np.float32(eps)), float(np.float32(scale)))
+    plain = wide(plain_f32(G, steps, f32(coeffs), float(np.float32(eps)), scale))
+    size = np.linalg.norm(want)
+    rounding = torch.finfo(dtype).eps / 2 * size + HALF_SUBNORMAL[dtype] * np.sqrt(want.size)
+    err = np.linalg.norm(wide(got) - want)
+    assert err <= 8 * np.linalg.norm(plain - want) + (2.0 ** -20 + carried) * size + rounding, (err / size, np.linalg.norm(plain - want) / size)
+
+
+@pytest.mark.parametrize("ratio", (0.3, 2.0 ** -6, 1e-4, 1e-6, 1e-9, 1e-20))
+@pytest.mark.parametrize("shape", SMALL)
+def test_an_update_far_below_eps(B, shape, ratio):
+    """||G|| = ratio * eps: X_0 is that small, and the steps enlarge it by up to a each.  Nothing of its 22 bits may be lost."""
+    G = torch.from_numpy(dense(shape, 6, 1.0)).cuda()
+    eps = float(np.float32(float(G.double().norm()) / ratio))
+    for steps in (1, 5):
+        near(B.gnnpre_orthogonalize(G, steps=steps, eps=eps, scale=0.7), G, steps, QUINTIC, eps, 0.7, F32)
+    if ratio <= 1e-4:  # steps enough to bring it to one
+        steps = 5 + int(np.log(1 / ratio) / np.log(3.4445))
+        near(B.gnnpre_orthogonalize(G, steps=steps, eps=eps), G, steps, QUINTIC, eps, 1.0, F32)
+
+
+@pytest.mark.parametrize("dtype", (BF16, F16))
+@pytest.mark.parametrize("ratio", (1e-2, 1e-6))
+def test_an_update_far_below_eps_whose_steps_are_multiplied_together(B, dtype, ratio):
+    G = torch.from_numpy(dense((300, 4000), 7, 1.0)).cuda().to(dtype)
+    eps = float(np.float32(float(G.double().norm()) / ratio))
+    for steps in (2, 3, 5, 12):
+        scale = 1.0 if steps > 5 else 1.0 / ratio  # (so that fp16 holds the result)
+        carried = -(-steps // 3) * 2.0 ** -11 if dtype is BF16 else -(-steps // 2) * 2.0 ** -14
+        near(B.gnnpre_orthogonalize(G, steps=steps, eps=eps, scale=scale), G, steps, QUINTIC, eps, scale, dtype, carried)
+
+
+@pytest.mark.parametrize("shape", [(100, 60), (300, 500), (1500, 1600)])
+def test_matrices_of_a_batch_lie_at_their_own_distance_from_eps(B, shape):
+    G = torch.from_numpy(dense((4, *shape), 8, 1.0)).cuda() * torch.tensor([1.0, 1e-3, 1e-7, 0.0], device="cuda")[:, None, None]
+    eps = float(np.float32(1e-2 * float(G[0].double().norm())))
+    out = B.gnnpre_orthogonalize(G, eps=eps)
+    for i in range(3):
+        near(out[i], G[i], 5, QUINTIC, eps, 1.0, F32)
+        assert torch.equal(out[i], B.gnnpre_orthogonalize(G[i], eps=eps)) or shape == (1500, 1600)  # (there tiles go by the batch)
+    assert (out[3] == 0).all()
+
+
+@pytest.mark.parametrize("coeffs,steps", [((0.01, 0.0, 0.0), 5), ((0.1, -0.05, 0.01), 8), ((0.0, 0.5, 0.0), 3), ((0.3, 0.0, 0.1), 6), ((0.0, 0.0, 0.0), 2)])
+@pytest.mark.parametrize("shape", SMALL)
+def test_coefficients_that_shrink_the_update(B, shape, coeffs, steps):
+    """Within the recurrence of the worst case that test_dense computes (X' = A X / 2 three times is a 27th power: it enlarges what X_0 is
+    off by as many times, which plain fp32 shows as well as these operands' 22 bits do)."""
+    G = torch.from_numpy(dense(shape, 9, 1.0)).cuda()
+    c = f32(coeffs)
+    want = orc.orthogonalize(wide(G), steps, c, float(np.float32(1e-7)), 1.0)
+    X = wide(G)
+    s = np.linalg.svd(X / np.sqrt((X ** 2).sum()), compute_uv=False)
+    off = 2.0 ** -22
+    for _ in range(steps):
+        top = (s * s).max()
+        off = slope(top, c) * off + (8 * 2.0 ** -22 + max(shape) * 2.0 ** -24) * size(top, c) * np.sqrt((s ** 2).sum())
+        s = s * np.abs(c[0] + c[1] * s ** 2 + c[2] * s ** 4)
+    assert np.linalg.norm(wide(B.gnnpre_orthogonalize(G, steps=steps, coeffs=coeffs)) - want) <= off + 2.0 ** -24 * np.linalg.norm(want)
