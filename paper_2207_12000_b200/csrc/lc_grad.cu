@@ -20,9 +20,10 @@
 //                boundaries take 4-byte copies by warps 24 and 25.
 //   warp 27      issues the products.
 //
-// Numbers.  An fp32 operand is the sum of three bf16 numbers, cut one after the other from its 24 bits, so nothing is lost and any
-// scale fits; of the nine products the six largest are taken, which drops less than 2^-23 of |dZ||X| per term.  (Two fp16 numbers
-// and three products would need a scale known before the data is read.)
+// Numbers.  An fp32 operand is the sum of three bf16 numbers h + m + l, each what is left rounded to nearest, so nothing is lost and
+// any scale fits; of the nine products the six largest are taken.  |m| <= 2^-8 and |l| <= 2^-17 of the operand, so those left out come to
+// 2^-24 of |dZ||X| per term at most, of either sign.  (Parts cut from the 24 bits, at the same number of instructions, leave out up to
+// 2^-21, and all of it has the product's sign.  Two fp16 numbers and three products would need a scale known before the data is read.)
 //
 // Tensor memory: two accumulators of 128 columns in turn, then 24 columns (three parts of 8: two elements of K per column) for each of
 // six chunks of A.  What A takes there it neither writes to nor is read from shared memory, whose bandwidth B alone then needs.
@@ -87,20 +88,26 @@ struct GradArgs {
     int32_t drop;               // self-test: chunks that are complete are not announced
 };
 
-// v = h + m + l, each with the upper 16 bits of an fp32 number only.
+// Two numbers in three bf16 parts each, the first one's in the lower halves.  Every part is rounded to nearest, and the third one holds
+// what is left exactly.
 struct Parts {
     uint32_t h, m, l;
 };
-__device__ __forceinline__ Parts cut(float v) {
-    Parts p;
-    p.h = __float_as_uint(v);
-    const float r = v - __uint_as_float(p.h & 0xffff0000u);
-    p.m = __float_as_uint(r);
-    p.l = __float_as_uint(r - __uint_as_float(p.m & 0xffff0000u));
+__device__ __forceinline__ uint32_t round2(float v, float w) {
+    uint32_t p;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p) : "f"(w), "f"(v));
     return p;
 }
-// The upper halves of two numbers, the first one low.
-__device__ __forceinline__ uint32_t pack(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
+__device__ __forceinline__ Parts split2(float v, float w) {
+    Parts p;
+    // (saturated: the largest fp32 numbers would round to infinity; of an infinity the second part is one and the third NaN)
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(p.h) : "f"(w), "f"(v));
+    v -= __uint_as_float(p.h << 16);
+    w -= __uint_as_float(p.h & 0xffff0000u);
+    p.m = round2(v, w);
+    p.l = round2(v - __uint_as_float(p.m << 16), w - __uint_as_float(p.m & 0xffff0000u));
+    return p;
+}
 
 template <int REGS>
 __device__ __forceinline__ void more_registers() {
@@ -265,10 +272,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
             uint32_t p[3][kGradChunk / 2];
 #pragma unroll
             for (int j = 0; j < kGradChunk / 2; ++j) {
-                const Parts e = cut(v[2 * j]), o = cut(v[2 * j + 1]);
-                p[0][j] = pack(e.h, o.h);
-                p[1][j] = pack(e.m, o.m);
-                p[2][j] = pack(e.l, o.l);
+                const Parts two = split2(v[2 * j], v[2 * j + 1]);
+                p[0][j] = two.h;
+                p[1][j] = two.m;
+                p[2][j] = two.l;
             }
             if (!tc_wait_warp(empty(s), ((uint32_t)(c / kGradStages) & 1u) ^ 1u, abort_flag, a.error, a.spin_limit)) break;
             tc_fence_after();
@@ -304,11 +311,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) k_lc_grad(const __grid_consta
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const int k = first_row + i;
-                const Parts x = cut(v[i].x), y = cut(v[i].y), z = cut(v[i].z), u = cut(v[i].w);
+                const Parts x = split2(v[i].x, v[i].y), z = split2(v[i].z, v[i].w);
                 const uint32_t at = to + 128u * k + ((uint32_t)((col % 64 / 8) ^ (k & 7)) << 4);
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(pack(x.h, y.h)), "r"(pack(z.h, u.h)) : "memory");
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + kGradPart), "r"(pack(x.m, y.m)), "r"(pack(z.m, u.m)) : "memory");
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + 2 * kGradPart), "r"(pack(x.l, y.l)), "r"(pack(z.l, u.l)) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x.h), "r"(z.h) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + kGradPart), "r"(x.m), "r"(z.m) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + 2 * kGradPart), "r"(x.l), "r"(z.l) : "memory");
             }
             tc_fence_async();
             __syncwarp();

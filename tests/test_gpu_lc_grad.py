@@ -225,3 +225,28 @@ def test_int64_indices_beyond_32_bits_are_padding(B):
     dY = rng.integers(-3, 4, size=(1, batch.size, H)).astype(np.float32)
     got = B.gnnpre_lc_first_layer_grad([aligned(hop)], torch.from_numpy(batch).cuda(), torch.from_numpy(dY).cuda())
     assert np.array_equal(got.cpu().double().numpy(), orc.lc_first_layer_grad([hop], batch, dY, None, 0))
+
+
+def test_one_term_is_off_by_little_more_than_a_rounding(B):
+    """A batch of one row: every element of the gradient is one product of two 24-bit numbers.  The products left out are below 2^-24 of
+    it; of the six sums inside the tensor core only the last is of the result's size, and cut at 2^-23 of it: 2^-22 covers both."""
+    rng = np.random.default_rng(2)
+    F, H = 1000, 256
+    x = (rng.choice([-1, 1], F) * (1 + rng.random(F)) * 2.0 ** rng.integers(-30, 30, F)).astype(np.float32)
+    dy = (rng.choice([-1, 1], H) * (1 + rng.random(H)) * 2.0 ** rng.integers(-30, 30, H)).astype(np.float32)
+    x[:8] = dy[:8] = [np.float32(1 + 2.0 ** -7 - 2.0 ** -23 * k) for k in range(1, 9)]  # long second and third parts
+    x[8:16] = dy[8:16] = [np.float32(1 + 2.0 ** -8 + 2.0 ** -16 + s * 2.0 ** -23) for s in range(-4, 4)]
+    got = B.gnnpre_lc_first_layer_grad([aligned(x[None])], None, torch.from_numpy(dy.reshape(1, 1, H)).cuda())
+    want = np.outer(dy.astype(np.float64), x.astype(np.float64))
+    off = np.abs(got.cpu().double().numpy() - want) / np.abs(want)
+    assert off.max() <= 2.0 ** -22, off.max() * 2.0 ** 23
+
+
+def test_the_largest_numbers_are_finite(B):
+    top = np.finfo(np.float32).max
+    x = np.array([[top, -top, 3.39e38, 3.3953e38, -3.38953e38, 1.0, 2.0 ** -100, 0.0]], dtype=np.float32)
+    dy = np.zeros((1, 1, 16), dtype=np.float32)
+    dy[0, 0, :4] = [1.0, -1.0, 0.5, 2.0 ** -20]
+    got = B.gnnpre_lc_first_layer_grad([torch.from_numpy(x).cuda()], None, torch.from_numpy(dy).cuda()).cpu().double().numpy()
+    want = np.outer(dy[0, 0].astype(np.float64), x[0].astype(np.float64))
+    assert (np.abs(got - want) <= 2.0 ** -22 * np.abs(want)).all()
