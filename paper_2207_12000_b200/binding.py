@@ -377,6 +377,11 @@ def _int32_rows(batch: torch.Tensor, n: int, stream) -> torch.Tensor:
         return batch.clamp(-1, n).to(torch.int32)
 
 
+def _hop_pitch(n: int, F: int, pitch: int) -> int:
+    """Leading dimension of hop matrices; a matrix of one row may have any, so it gets one that the library takes."""
+    return pitch if n > 1 else (F + 3) // 4 * 4
+
+
 def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, precision: int = GNNPRE_LC_TF32,
                           out: torch.Tensor | None = None,
                           concat: bool = False, check: bool = True, stream=None) -> torch.Tensor:
@@ -411,7 +416,7 @@ def gnnpre_lc_first_layer(hops, batch, Wt: torch.Tensor, *, relu_mask: int = 0, 
         assert out.shape == (K, B, H) and os[2] == 1
         ldy, hop_stride = (os[1], os[0]) if B > 0 else (H, 0)
     flag = _error_word(Wt.device, stream) if check else None
-    _check(_lib.gnnpre_lc_first_layer(_pointers(hops), K, n, F, hs[0], bptr, B, Wt.data_ptr(), H, ws[0],
+    _check(_lib.gnnpre_lc_first_layer(_pointers(hops), K, n, F, _hop_pitch(n, F, hs[0]), bptr, B, Wt.data_ptr(), H, ws[0],
                                       relu_mask, precision, out.data_ptr(), ldy, hop_stride,
                                       flag.data_ptr() if check else None, _stream_ptr(stream)), "gnnpre_lc_first_layer")
     if check:
@@ -550,7 +555,7 @@ def gnnpre_lc_first_layer_grad(hops, batch, dY: torch.Tensor, *, Y: torch.Tensor
     room = _workspace(workspace, _lib.gnnpre_lc_first_layer_grad_workspace(K, N, F, H), "gnnpre_lc_first_layer_grad", dY.device, stream)
     assert room.get_device() == device
     flag = _error_word(dY.device, stream) if check else None
-    _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, hs[0], bptr, N, dY.data_ptr(), *layout[0],
+    _check(_lib.gnnpre_lc_first_layer_grad(_pointers(hops), K, n, F, _hop_pitch(n, F, hs[0]), bptr, N, dY.data_ptr(), *layout[0],
                                            Y.data_ptr() if Y is not None else None, *layout[1], relu_mask, H, int(accumulate), out.data_ptr(),
                                            ldw, room.data_ptr(), room.numel(), flag.data_ptr() if check else None,
                                            _raw_stream(device) if stream is None else stream.cuda_stream), "gnnpre_lc_first_layer_grad")

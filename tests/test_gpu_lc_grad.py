@@ -250,3 +250,13 @@ def test_the_largest_numbers_are_finite(B):
     got = B.gnnpre_lc_first_layer_grad([torch.from_numpy(x).cuda()], None, torch.from_numpy(dy).cuda()).cpu().double().numpy()
     want = np.outer(dy[0, 0].astype(np.float64), x[0].astype(np.float64))
     assert (np.abs(got - want) <= 2.0 ** -22 * np.abs(want)).all()
+
+
+def test_hops_of_one_node(B):
+    """A matrix of one row has no pitch to speak of: torch may say 0, or the length of an odd row."""
+    dY = torch.ones((1, 1, 16), device="cuda")
+    for F in (1, 7, 100, 602):
+        x = torch.arange(1, F + 1, device="cuda", dtype=torch.float32)
+        for hop in (x[None], x[None].expand(1, F), x.as_strided((1, F), (0, 1))):
+            got = B.gnnpre_lc_first_layer_grad([hop], None, dY)
+            assert torch.equal(got, x.expand(16, F))

@@ -268,3 +268,12 @@ def test_int64_indices_beyond_32_bits_are_padding(B):
     for precision in (B.GNNPRE_LC_TF32, B.GNNPRE_LC_TF32X3):
         Y = B.gnnpre_lc_first_layer([hop], batch, Wt, precision=precision)
         assert Y[0, :, 0].tolist() == [20, 0, 20, 0, 0, 0, 20, 0, 0]
+
+
+def test_hops_of_one_node(B):
+    """A matrix of one row has no pitch to speak of: torch may say 0, or the length of an odd row."""
+    for F in (1, 7, 100, 602):
+        x = torch.ones(F, device="cuda")
+        Wt = padded_cuda(np.ones((16, F), dtype=np.float32), 0)
+        for hop in (x[None], x.as_strided((1, F), (0, 1))):
+            assert (B.gnnpre_lc_first_layer([hop], None, Wt) == F).all()
