@@ -215,3 +215,29 @@ def test_rows_of_a_table_beyond_32_bit_offsets(B):
     B.gnnpre_embedding_grad(values, ids, rows, out=table)
     assert torch.equal(table[rows - 1], values[0]) and torch.equal(table[0], values[1]) and torch.equal(table[rows - 2], values[2])
     assert int(torch.count_nonzero(table[1:rows - 2])) == 0
+
+
+@pytest.mark.parametrize("dtype,to", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("rows,dim,count,how", [
+    (3000, 8, 262_145, "mixed"), (3000, 20, 524_289, "mixed"), (100, 12, 606_208, "uniform"), (100, 12, 606_209, "uniform"),
+    (70_000, 16, 700_001, "mixed"), (5_000_000, 4, 1_000_003, "mixed"), (2, 33, 800_000, "one"), (40, 6, 650_000, "padding"),
+    (1000, 8, 2_100_000, "descending"), (300, 130, 620_000, "mixed")])
+def test_grad_of_long_lists_is_exact_on_integers(B, rows, dim, count, how, dtype, to):
+    """Segments of 64 and 128 entries, and blocks of 4,096 keys in the sort (from 606,209 ids on), in one to three passes.  In 16 bits the
+    d_out of all but a few positions of a row are zero, so that its sum is still a small integer."""
+    d_out = matrix(count, dim, dtype, 3, integers=True)
+    if to is not F32:
+        d_out[torch.rand(count, generator=torch.Generator().manual_seed(1)).cuda() < 1 - 20 * min(rows, 1000) / count] = 0
+        d_out.clamp_(-1, 1)
+    ids, ids_np = draw_ids(count, rows, how, count + 1, torch.int32 if count % 2 else torch.int64)
+    known = (ids >= 0) & (ids < rows)
+    want = torch.zeros((rows, dim), dtype=torch.float64, device="cuda").index_add_(0, ids[known].long(), d_out[known].double())
+    if to is not F32 and float(want.abs().max()) > 256:
+        d_out[:] = 0  # (one row takes everything: 200 positions of it)
+        d_out[::count // 200] = 1
+        want = torch.zeros((rows, dim), dtype=torch.float64, device="cuda").index_add_(0, ids[known].long(), d_out[known].double())
+    out = B.gnnpre_embedding_grad(d_out, ids, rows, scale=2.0, out=torch.full((rows, dim), float("nan"), dtype=to, device="cuda"))
+    assert torch.equal(out.double(), 2 * want)
+    old = matrix(rows, dim, to, 4, integers=True)
+    again = B.gnnpre_embedding_grad(d_out, ids, rows, scale=-2.0, out=old.clone(), accumulate=True)
+    assert torch.equal(again.double(), (old.double() - 2 * want).to(to).double())

@@ -260,3 +260,39 @@ def test_hops_of_one_node(B):
         for hop in (x[None], x[None].expand(1, F), x.as_strided((1, F), (0, 1))):
             got = B.gnnpre_lc_first_layer_grad([hop], None, dY)
             assert torch.equal(got, x.expand(16, F))
+
+
+@pytest.mark.parametrize("pad", (0, 4, 3))
+@pytest.mark.parametrize("n,F,H,bs,K", [(700, 36, 16, 300, 2), (700, 130, 48, 299, 3), (500, 20, 144, 1000, 9), (900, 100, 256, 777, 3), (90, 8, 256, 1, 2)])
+def test_layouts_of_the_gradient_are_exact_on_integers(B, n, F, H, bs, K, pad):
+    """[K, B, H] and hops side by side, rows that start on 16-byte boundaries (pad 0 and 4: the copy engine's tiles, whose outermost stride
+    is then smaller than a row) and rows that do not; padding rows and masked elements hold what must not be looked at."""
+    hops, batch, dY, Y = case(n, F, H, bs, K, n + F + pad, True)
+    mask = 0b101010110
+    for k in range(K):
+        if mask >> k & 1:
+            dY[k][(Y[k] <= 0) & np.isfinite(dY[k])] = np.inf
+    with np.errstate(invalid="ignore"):
+        want = orc.lc_first_layer_grad(hops, batch, dY, Y, mask)
+    d_hops, d_batch = [aligned(h) for h in hops], torch.from_numpy(batch).cuda()
+    place = (lambda M: padded(M, pad)) if pad else (lambda M: torch.from_numpy(np.ascontiguousarray(M)).cuda())
+    got = B.gnnpre_lc_first_layer_grad(d_hops, d_batch, place(dY), Y=place(Y), relu_mask=mask)
+    assert np.array_equal(got.cpu().double().numpy(), want)
+    side = [np.concatenate(list(t), axis=1) for t in (dY, Y)]
+    got = B.gnnpre_lc_first_layer_grad(d_hops, d_batch, place(side[0]), Y=place(side[1]), relu_mask=mask, concat=True)
+    assert np.array_equal(got.cpu().double().numpy(), want)
+
+
+@pytest.mark.parametrize("K,H", [(1, 64), (2, 16), (3, 144), (9, 256)])
+def test_the_forward_calls_own_output_side_by_side(B, K, H):
+    rng = np.random.default_rng(K)
+    hops = [rng.integers(-2, 3, size=(600, 24)).astype(np.float32) for _ in range(K)]
+    batch = rng.integers(-1, 600, size=433)
+    Wt = rng.integers(-2, 3, size=(H, 24)).astype(np.float32)
+    mask = (1 << K) - 2
+    d_hops, d_batch = [aligned(h) for h in hops], torch.from_numpy(batch).cuda()
+    Y = B.gnnpre_lc_first_layer(d_hops, d_batch, torch.from_numpy(Wt).cuda(), relu_mask=mask, concat=True)
+    dY = rng.integers(-3, 4, size=(433, K * H)).astype(np.float32)
+    got = B.gnnpre_lc_first_layer_grad(d_hops, d_batch, torch.from_numpy(dY).cuda(), Y=Y, relu_mask=mask, concat=True)
+    split = lambda M: list(M.reshape(433, K, H).transpose(1, 0, 2))  # noqa: E731
+    assert np.array_equal(got.cpu().double().numpy(), orc.lc_first_layer_grad(hops, batch, split(dY), split(Y.cpu().numpy()), mask))

@@ -342,3 +342,62 @@ def test_coefficients_that_shrink_the_update(B, shape, coeffs, steps):
         off = slope(top, c) * off + (8 * 2.0 ** -22 + max(shape) * 2.0 ** -24) * size(top, c) * np.sqrt((s ** 2).sum())
         s = s * np.abs(c[0] + c[1] * s ** 2 + c[2] * s ** 4)
     assert np.linalg.norm(wide(B.gnnpre_orthogonalize(G, steps=steps, coeffs=coeffs)) - want) <= off + 2.0 ** -24 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16, F16))
+@pytest.mark.parametrize("shape", [
+    (3, 1000, 777), (2, 600, 2500), (4, 2500, 300), (2, 1500, 1600), (7, 256, 602), (9, 602, 256), (7, 384, 1024), (8, 1024, 384),
+    (2, 128, 2048), (2, 2048, 128), (3, 100, 1100), (3, 600, 100), (40, 60, 257), (6, 384, 1024), (2, 20, 40000), (1, 3000, 70)])
+def test_batches_of_every_form(B, shape, dtype):
+    """Several matrices at once, by a launch per product (steps by themselves and multiplied together), by clusters of 8 and of 16 CTAs with
+    up to all the tiles they hold, on the chip by one to eight CTAs: each matrix as near the oracle as plain fp32 is."""
+    G = torch.from_numpy(dense(shape, sum(shape))).cuda().to(dtype)
+    out = B.gnnpre_orthogonalize(G, scale=0.9)
+    r, n = sorted(shape[1:])
+    alone = r > 128 or n > 2048
+    carried = {F32: 0.0, BF16: 2 * 2.0 ** -11, F16: 3 * 2.0 ** -14}[dtype] if alone else 0.0
+    for i in range(0, shape[0], max(1, shape[0] // 4)):
+        near(out[i], G[i], 5, QUINTIC, 1e-7, 0.9, dtype, carried)
+    if not alone:  # on the chip nothing depends on how many there are
+        assert torch.equal(out[-1], B.gnnpre_orthogonalize(G[-1], scale=0.9))
+    assert torch.equal(B.gnnpre_orthogonalize(G, scale=0.9), out)
+
+
+@pytest.mark.parametrize("shape", [(64, 128), (300, 500), (1300, 1290)])
+def test_weak_values_beside_strong_ones(B, shape):
+    """One value per row and column, from 1 to 2^-36 of the largest: below some 2^-16 an operand's entry is off by 2^-39 of the bound (two,
+    here) instead of 2^-22 of itself, in every X that is held; the rest as in test_one_value_per_row_and_column."""
+    rng = np.random.default_rng(4)
+    r = min(shape)
+    i, j = rng.permutation(shape[0])[:r], rng.permutation(shape[1])[:r]
+    G = np.zeros(shape, dtype=np.float32)
+    G[i, j] = 2.0 ** -(36 * np.arange(r) / r) * rng.choice([-1, 1], r)
+    got = wide(B.gnnpre_orthogonalize(torch.from_numpy(G).cuda()))
+    c = f32(QUINTIC)
+    s = np.abs(G[i, j].astype(np.float64))
+    s = s / (np.sqrt((s ** 2).sum()) + float(np.float32(1e-7)))
+    err = 2.0 ** -22 * s + 2.0 ** -38
+    for _ in range(5):
+        t = s * s
+        err = slope(t, c) * err + 8 * 2.0 ** -22 * s * size(t, c) + 2.0 ** -38
+        s = s * (c[0] + c[1] * t + c[2] * t * t)
+    want = s * np.sign(G[i, j])
+    assert (np.abs(got[i, j] - want) <= err + 2.0 ** -24 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("shape", [(100, 60), (100, 900), (300, 700), (1500, 1600)])
+def test_replayed_and_after_waits_that_ran_out_it_is_as_exact_as_ever(B, shape):
+    G, out = torch.zeros(shape, device="cuda"), torch.empty(shape, device="cuda")
+    room = torch.empty(B.gnnpre_orthogonalize_workspace(1, *shape, 5), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    B.gnnpre_orthogonalize(G, out=out, workspace=room)
+    with torch.cuda.graph(graph):
+        B.gnnpre_orthogonalize(G, out=out, workspace=room, check=False)
+    for seed in (1, 2):
+        G.copy_(torch.from_numpy(dense(shape, seed)).cuda())
+        room.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        near(out, G, 5, QUINTIC, 1e-7, 1.0, F32)
+    assert B.gnnpre_orthogonalize_selftest_wait_timeout(G, polls=50) == -8
+    assert torch.equal(B.gnnpre_orthogonalize(G), out)
