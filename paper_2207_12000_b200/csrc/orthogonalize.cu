@@ -616,7 +616,7 @@ constexpr int kClusterStages = 3;
 constexpr int kClusterStaging = 2 * kBlockBytes;                         // a tile and its transpose
 constexpr int kClusterSmem = kClusterStages * (int)kClusterStage + kClusterStaging + 1024;
 constexpr int kClusterSourceTiles = (kClusterSmem - 1024) / (64 * 65 * 4);
-constexpr int kMostClusterTiles = 48;   // tiles of X in a product, at most
+constexpr int kMostClusterTiles = 32;   // tiles of X in a product, at most
 static_assert(2 * kMostClusterTiles / 8 <= kClusterSourceTiles, "the [64, 64] tiles of X that a CTA reads fit");
 
 __device__ __forceinline__ void ns_cluster_sync() {
@@ -1385,9 +1385,14 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     s.np = (s.n + 127) / 128 * 128;
     // multiplications per step of a segment of g steps, in units of r^2: n + 2 n for its ends, (4 g - 3) r between
     const auto cost = [&](int g) { return (3.0 * s.np + (4.0 * g - 3.0) * s.rp) / g; };
-    // One cluster per matrix while a CTA of it has few tiles in a product.
+    // One cluster per matrix where the square products leave a CTA one tile (r <= 256, eight tiles) and those of X few, and where all
+    // matrices' clusters run at once: seven of 16 CTAs, fourteen of 8.  us, fp32, five steps, 16 CTAs / 8 / a launch per product:
+    // one of 200 x 384 110 / 127 / 121, 256 x 512 117 / 137 / 128, 256 x 1,024 165 / 204 / 160; seven of them 111 / 128 / 126, 118 / 137 /
+    // 135, 166 / 205 / 182; ten of 256 x 512 234 / 138 / 150, sixteen 350 / 273 / 155; one of 130 x 130 90 / 93 / 100.  Beyond: 256 x 1,536
+    // 213 / 271 / 192, 384 x 384 194 / 266 / 138, 300 x 1,000 276 / 421 / 169.
     const int64_t tiles = s.rp / 128 * (s.np / kClusterTile);
-    s.ctas = tiles > kMostClusterTiles ? 0 : tiles > 8 && batch <= 6 ? 16 : 8;
+    const bool cluster = s.rp <= 256 && tiles <= kMostClusterTiles && batch <= 14;
+    s.ctas = !cluster ? 0 : tiles > 8 && batch <= 7 ? 16 : 8;
     s.chip = s.r <= 128 && s.n <= kChipCols * kChipMaxCtas;
     if (s.chip)
         for (s.ctas = 1; s.ctas * kChipCols < s.n;) s.ctas *= 2;

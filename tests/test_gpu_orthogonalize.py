@@ -401,3 +401,15 @@ def test_replayed_and_after_waits_that_ran_out_it_is_as_exact_as_ever(B, shape):
         near(out, G, 5, QUINTIC, 1e-7, 1.0, F32)
     assert B.gnnpre_orthogonalize_selftest_wait_timeout(G, polls=50) == -8
     assert torch.equal(B.gnnpre_orthogonalize(G), out)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("shape", [(7, 256, 1000), (8, 256, 1000), (14, 200, 384), (15, 200, 384), (12, 384, 130), (16, 130, 130), (1, 257, 257), (3, 256, 1030)])
+def test_both_sides_of_where_clusters_end(B, shape, dtype):
+    """Clusters of 16 CTAs up to seven matrices, of 8 up to fourteen, for a smaller side of at most 256 and 32 tiles; a launch per product
+    beyond."""
+    G = torch.from_numpy(dense(shape, 2)).cuda().to(dtype)
+    out = B.gnnpre_orthogonalize(G)
+    carried = 0.0 if dtype is F32 else 2 * 2.0 ** -11
+    for i in {0, shape[0] // 2, shape[0] - 1}:
+        near(out[i], G[i], 5, QUINTIC, 1e-7, 1.0, dtype, carried)
