@@ -316,7 +316,7 @@ struct Product {
 //
 // The tensor core cuts, not rounds, a sum that it adds a product to: over K = 4000 in one accumulator the sums of squares in A
 // came out 1e-5 too small (750 additions, half of 2^-23 each).  So an accumulator takes one chunk only, its small terms first, so
-// that four cuts count; two take turns, and their sums are added up in registers, rounded to nearest, while the next ones form.
+// that four cuts count; four take turns (two of 256 columns), and their sums are added up in registers, rounded to nearest, while the next ones form.
 // What bounds a wide product is shared memory: per 64 of K a 128 x 128 tile writes 64 KB and the twelve products read 96 KB, 1,280 cycles at
 // 128 bytes a cycle for 840 of the tensor core; 128 x 256 takes 1,920 for twice the work.
 template <int BN>
@@ -1393,7 +1393,10 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     const int64_t tiles = s.rp / 128 * (s.np / kClusterTile);
     const bool cluster = s.rp <= 256 && tiles <= kMostClusterTiles && batch <= 14;
     s.ctas = !cluster ? 0 : tiles > 8 && batch <= 7 ? 16 : 8;
-    s.chip = s.r <= 128 && s.n <= kChipCols * kChipMaxCtas;
+    // On the chip where a matrix fits, and where eight CTAs are needed while all matrices' clusters run at once (else as above).  us, on
+    // the chip / a launch per product: one of 64 x 64 35 / 77, 128 x 256 54 / 96, 128 x 1,000 101 / 144, 128 x 2,048 176 / 207; fourteen of
+    // the last 199 / 269, eighteen 361 / 275; a hundred of 128 x 256 56 / 198, of 128 x 1,000 421 / 478.
+    s.chip = s.r <= 128 && s.n <= kChipCols * kChipMaxCtas && (batch <= 14 || 2 * s.n <= kChipCols * kChipMaxCtas);
     if (s.chip)
         for (s.ctas = 1; s.ctas * kChipCols < s.n;) s.ctas *= 2;
     s.segment = 1;
@@ -1476,7 +1479,8 @@ int launch_product_n(const Product& a, int64_t tiles_m, int64_t batch, cudaStrea
 // D has rows x cols elements.
 int launch_product(Product& a, int64_t rows, int64_t cols, int64_t batch, bool symmetric, int sms, cudaStream_t st) {
     const int64_t tiles_m = rows / 128;
-    // Tiles of 128 x 64 while they fit the machine; symmetric products need square ones to leave any out.
+    // Tiles of 128 x 64 while they fit the machine; symmetric products need square ones to leave any out.  us, one matrix, never / so /
+    // up to twice as many: 500 x 1,000 262 / 195 / 195, 1,000 x 1,000 341 / 264 / 264, 1,024 x 2,048 420 / 352 / 411, 1,500 x 1,500 466 / 466 / 710.
     const bool narrow = tiles_m * (cols / 64) * batch * a.jobs <= sms;
     a.symmetric = symmetric && !narrow && tiles_m > 1;
     // Tiles of 128 x 256 where they give every SM one (2,048 x 4,096, five steps: 1,340 us without them, 1,216 with).

@@ -413,3 +413,12 @@ def test_both_sides_of_where_clusters_end(B, shape, dtype):
     carried = 0.0 if dtype is F32 else 2 * 2.0 ** -11
     for i in {0, shape[0] // 2, shape[0] - 1}:
         near(out[i], G[i], 5, QUINTIC, 1e-7, 1.0, dtype, carried)
+
+
+@pytest.mark.parametrize("shape", [(14, 1100, 40), (15, 40, 1100), (15, 1024, 100), (100, 30, 70)])
+def test_many_small_matrices(B, shape):
+    """Up to fourteen by eight CTAs each on the chip, more of them by a launch per product; any number by up to four CTAs."""
+    G = torch.from_numpy(dense(shape, 3)).cuda()
+    out = B.gnnpre_orthogonalize(G)
+    for i in (0, shape[0] // 2, shape[0] - 1):
+        near(out[i], G[i], 5, QUINTIC, 1e-7, 1.0, F32)
