@@ -451,13 +451,15 @@ def gnnpre_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: fl
                             stream=None) -> torch.Tensor:
     """scale * table[ids] ([N, D]); an id outside the table (padding) gives a row of zeros.
 
-    table: device fp32, bf16 or fp16 [V, D] with stride(1) == 1; ids: device int32 or int64 [N]; out: of table's type."""
+    table: device fp32, bf16 or fp16 [V, D] with stride(1) == 1; ids: device int32 or int64 [N]; out: of table's type, by default with
+    rows that start on 16-byte boundaries, as gnnpre_propagate and gnnpre_lc_first_layer want them."""
     V, D = table.shape
     (N,) = ids.shape
     dtype, id_type = _DTYPES.get(table.dtype), _ID_TYPES.get(ids.dtype)
     assert dtype is not None and id_type is not None and ids.is_contiguous()
     if out is None:
-        out = _result((N, D), table.dtype, table.device, stream)
+        whole = 16 // table.element_size()
+        out = _result((N, (D + whole - 1) // whole * whole), table.dtype, table.device, stream)[:, :D]
     (ldt, one), (ldo, also_one) = table.stride(), out.stride()
     assert out.dtype is table.dtype and out.shape == (N, D) and (D == 1 or one == 1 == also_one)
     # (the library launches on the current device's stream: operands of another device, or of the host, are refused)

@@ -241,3 +241,24 @@ def test_grad_of_long_lists_is_exact_on_integers(B, rows, dim, count, how, dtype
     old = matrix(rows, dim, to, 4, integers=True)
     again = B.gnnpre_embedding_grad(d_out, ids, rows, scale=-2.0, out=old.clone(), accumulate=True)
     assert torch.equal(again.double(), (old.double() - 2 * want).to(to).double())
+
+
+@pytest.mark.parametrize("dim", (602, 100, 7))
+def test_the_hops_take_what_a_lookup_makes(B, dim):
+    """The default result is X_0 of a graph as it is, whatever the table's width; 16-bit rows start on 16-byte boundaries too."""
+    n = 60
+    rowptr, colidx = torch.arange(n + 1, dtype=torch.int64, device="cuda"), ((torch.arange(n, device="cuda") + 1) % n).to(torch.int32)
+    table = matrix(20, dim, F32, 1, integers=True)
+    ids = torch.arange(n, device="cuda") % 20
+    X = B.gnnpre_embedding_lookup(table, ids)
+    assert X.shape == (n, dim) and torch.equal(X, table[ids])
+    plan = B.gnnpre_build_plan(rowptr, colidx, B.GNNPRE_OP_SAGE_MEAN, dim)
+    hops, _ = B.gnnpre_propagate(plan, X, 1)  # every node has one neighbour: the next one
+    assert torch.equal(hops[0], torch.roll(X, -1, 0))
+    Wt = matrix(16, dim, F32, 2, pad=-dim % 4, integers=True)
+    want = (X.double() @ Wt.double().T).float()
+    assert torch.equal(B.gnnpre_lc_first_layer([X], None, Wt, precision=B.GNNPRE_LC_TF32X3)[0], want)
+    for dtype in (BF16, F16):
+        rows = B.gnnpre_embedding_lookup(table.to(dtype), ids)
+        assert rows.stride(0) % 8 == 0 and torch.equal(rows.float(), X)
+    plan.close()
