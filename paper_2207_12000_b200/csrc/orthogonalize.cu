@@ -10,9 +10,10 @@
 // bits of entries down to some 2^-16 of the bound, and of smaller ones an absolute error of 2^-39 of it, far below that of fp32 sums of
 // that size.  (An update whose norm is far below eps starts far below one: the device finds bounds for it from its norm.)  A product
 // takes three tensor-core products (high x high, high x low, low x high) into one fp32 accumulator; what is dropped is below 2^-22 of
-// the operands.  fp16 carries
-// 11 bits where tf32 carries as many at half the rate and bf16 carries 8: one fp16 product in place of the three would lose the
-// small singular values, which a step multiplies by a (3.4) and with them the rounding errors of the large ones.
+// the operands.  fp16 carries 11 bits where tf32 carries as many at half the rate and bf16 carries 8: one fp16 product in place of
+// the three would lose the small singular values, which a step multiplies by a (3.4) and with them the rounding errors of the large
+// ones.  (Plain fp32 has 24 bits: it is off by 1.7e-6 on [256, 128] where this is by 1.9e-6, and by 4.6e-6 on [2048, 4096], whose long
+// sums it rounds more often, where this is by 1.6e-6.)
 //
 // Order of the products.  The polynomials of a few steps commute and are polynomials of the first A, so they can be multiplied
 // together before X: with P = aI + bA + cA^2, X <- P X makes A <- P A P.  A segment of g steps is
@@ -22,8 +23,8 @@
 // none of it: [256, 128] with six strong directions is off by 1.8e-6 in steps by themselves (as plain fp32 is) and by 2.0e-4 in
 // segments of three.  So segments have three steps at most for bf16 outputs (one rounding: 1.7e-3), two for fp16, one for fp32.
 //
-// Measured, us, five steps: 256 x 128 61 (one CTA, from shared memory), three of 256 x 602 144 (a cluster of 16 CTAs each), 2,048 x
-// 4,096 1,220 (a launch per product; 164-182 TFLOP/s of the least work, three times that on the tensor cores).
+// Measured, us, five steps: 256 x 128 59 (one CTA, from shared memory; 56-58 in a graph), three of 256 x 602 144 (a cluster of 16
+// CTAs each), 2,048 x 4,096 1,220 (a launch per product; 164-183 TFLOP/s of the least work, three times that on the tensor cores).
 //
 // Layout.  Operands are stored as the tensor core reads them: blocks of 128 rows x 64 columns of K in the 128-byte swizzle, the
 // high parts' 16 KB and then the low parts', so an operand tile is one contiguous copy and needs no tensor map.
