@@ -1392,8 +1392,8 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     // 135, 166 / 205 / 182; ten of 256 x 512 234 / 138 / 150, sixteen 350 / 273 / 155; one of 130 x 130 90 / 93 / 100.  Beyond: 256 x 1,536
     // 213 / 271 / 192, 384 x 384 194 / 266 / 138, 300 x 1,000 276 / 421 / 169.
     const int64_t tiles = s.rp / 128 * (s.np / kClusterTile);
-    const bool cluster = s.rp <= 256 && tiles <= kMostClusterTiles && batch <= 14;
-    s.ctas = !cluster ? 0 : tiles > 8 && batch <= 7 ? 16 : 8;
+    const bool ever_cluster = s.rp <= 256 && tiles <= kMostClusterTiles;  // (for some number of matrices)
+    s.ctas = !ever_cluster || batch > 14 ? 0 : tiles > 8 && batch <= 7 ? 16 : 8;
     // On the chip where a matrix fits, and where eight CTAs are needed while all matrices' clusters run at once (else as above).  us, on
     // the chip / a launch per product: one of 64 x 64 35 / 77, 128 x 256 54 / 96, 128 x 1,000 101 / 144, 128 x 2,048 176 / 207; fourteen of
     // the last 199 / 269, eighteen 361 / 275; a hundred of 128 x 256 56 / 198, of 128 x 1,000 421 / 478.
@@ -1419,7 +1419,8 @@ NsShape ns_shape(int64_t batch, int64_t rows, int64_t cols, int32_t steps, int32
     }
     s.x = take(s.side);
     s.xt[0] = take(s.side);
-    s.xt[1] = steps > s.segment || s.ctas ? take(s.side) : s.xt[0];
+    // (where a cluster may do it, as much for a launch per product: a kept workspace serves fewer matrices than it was made for)
+    s.xt[1] = steps > s.segment || ever_cluster ? take(s.side) : s.xt[0];
     s.a = take(s.square);
     s.a2 = take(s.square);
     s.p = take(s.square);

@@ -150,3 +150,13 @@ def test_lc_grad_looks_at_no_more_of_its_workspace_than_it_asks_for(lib):
     """An input behind the part that the call needs is none of its business: the call gets as far as asking for a device."""
     need = lib.gnnpre_lc_first_layer_grad_workspace(2, 100, 60, 32)
     assert call(lib.gnnpre_lc_first_layer_grad, LC_GRAD, dY=0x4000000 + need) not in (INVALID_ARG, ALIGN)
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 64), (100, 1100), (130, 130), (256, 1024), (256, 1030), (200, 300), (300, 500), (1500, 1600)])
+def test_orthogonalize_workspace_grows_with_the_batch(lib, rows, cols):
+    """One that is kept for so many matrices serves fewer, whichever form those take; and more steps ask for no less."""
+    size = lib.gnnpre_orthogonalize_workspace
+    for steps in (1, 2, 3, 5, 9):
+        sizes = [size(batch, rows, cols, steps) for batch in range(1, 40)]
+        assert all(0 < a <= b for a, b in zip(sizes, sizes[1:]))
+        assert sizes[-1] <= size(39, rows, cols, steps + 1)
