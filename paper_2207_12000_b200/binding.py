@@ -168,14 +168,19 @@ def _wait_for_current(stream) -> None:
         stream.wait_stream(torch.cuda.current_stream())
 
 
-def _result(shape, dtype, device, stream) -> torch.Tensor:
-    """A result that the caller did not bring, from the current stream's memory.  If the kernels run on another stream, that one waits for
-    the current one, whose work may still use the block, and the allocator is told of the use there."""
-    out = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and out.is_cuda:
+def _results(count: int, shape, dtype, device, stream) -> list[torch.Tensor]:
+    """Results that the caller did not bring, from the current stream's memory.  If the kernels run on another stream, that one waits for
+    the current one, whose work may still use the blocks, and the allocator is told of their use there."""
+    made = [torch.empty(shape, dtype=dtype, device=device) for _ in range(count)]
+    if stream is not None and made and made[0].is_cuda:
         _wait_for_current(stream)
-        out.record_stream(stream)
-    return out
+        for out in made:
+            out.record_stream(stream)
+    return made
+
+
+def _result(shape, dtype, device, stream) -> torch.Tensor:
+    return _results(1, shape, dtype, device, stream)[0]
 
 
 def _error_word(device, stream) -> torch.Tensor:
@@ -302,7 +307,7 @@ def gnnpre_propagate(plan: Plan, X: torch.Tensor, K: int, out: Sequence[torch.Te
     if out is None:
         Fp = (F + 3) // 4 * 4  # the library works on whole groups of 4 columns
         if on_device:
-            out = [_result((n, Fp), torch.float32, X.device, stream)[:, :F] for _ in range(K)]
+            out = [t[:, :F] for t in _results(K, (n, Fp), torch.float32, X.device, stream)]
         else:
             out = [torch.empty((n, Fp), dtype=torch.float32, pin_memory=True)[:, :F] for _ in range(K)]
     assert len(out) == K
@@ -353,7 +358,7 @@ def gnnpre_propagate_weighted(plan: Plan, X: torch.Tensor, gamma, *, out=None, Z
     Fp = (F + 3) // 4 * 4
     if out is None:
         nbuf = K if keep_hops else min(K, 2)
-        bufs = [_result((n, Fp), torch.float32, X.device, stream)[:, :F] for _ in range(nbuf)]
+        bufs = [t[:, :F] for t in _results(nbuf, (n, Fp), torch.float32, X.device, stream)]
         out = [bufs[k % nbuf] for k in range(K)]
     if Z is None:
         Z = _result((n, Fp), torch.float32, X.device, stream)[:, :F]
@@ -459,7 +464,9 @@ def gnnpre_embedding_lookup(table: torch.Tensor, ids: torch.Tensor, *, scale: fl
     assert dtype is not None and id_type is not None and ids.is_contiguous()
     if out is None:
         whole = 16 // table.element_size()
-        out = _result((N, (D + whole - 1) // whole * whole), table.dtype, table.device, stream)[:, :D]
+        out = _result((N, (D + whole - 1) // whole * whole), table.dtype, table.device, stream)
+        if D % whole:
+            out = out[:, :D]
     (ldt, one), (ldo, also_one) = table.stride(), out.stride()
     assert out.dtype is table.dtype and out.shape == (N, D) and (D == 1 or one == 1 == also_one)
     # (the library launches on the current device's stream: operands of another device, or of the host, are refused)
