@@ -157,15 +157,20 @@ def _stream_ptr(stream) -> int:
     return stream.cuda_stream
 
 
+def _torch_stream(stream):
+    """`stream` as torch's own, also where it is another library's object that has a handle only."""
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
 def _on(stream):
     """Where a call takes and fills what it makes for itself (workspace, converted indices, error word): on the stream that its kernels
     run on, whose order then covers a block from its last use to its next."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream))
 
 
 def _wait_for_current(stream) -> None:
     if stream is not None:
-        stream.wait_stream(torch.cuda.current_stream())
+        _torch_stream(stream).wait_stream(torch.cuda.current_stream())
 
 
 def _results(count: int, shape, dtype, device, stream) -> list[torch.Tensor]:
@@ -175,7 +180,7 @@ def _results(count: int, shape, dtype, device, stream) -> list[torch.Tensor]:
     if stream is not None and made and made[0].is_cuda:
         _wait_for_current(stream)
         for out in made:
-            out.record_stream(stream)
+            out.record_stream(_torch_stream(stream))
     return made
 
 

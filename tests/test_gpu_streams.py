@@ -103,3 +103,22 @@ def test_calls_on_two_streams_side_by_side(B):
             assert np.array_equal(wide(grads[i]), orc.embedding_grad(wide(d_out[i]), table_ids[i], rows, 1.0))
             assert np.array_equal(wide(weights[i]), wide(dY[i])[0].T @ wide(hop))
             assert torch.equal(updates[i], alone[i])
+
+
+def test_another_librarys_stream(B):
+    """An object that has a handle only: what the calls make is ordered with it as with torch's own."""
+    class Handle:
+        def __init__(self, cuda_stream):
+            self.cuda_stream = cuda_stream
+
+    side = torch.cuda.Stream()
+    table, ids, batch = integers(50, 12, seed=1), torch.arange(300, device="cuda") % 50, torch.arange(40, device="cuda")
+    G, dY = integers(30, 20, seed=2), integers(1, 40, 16, seed=3)
+    for stream in (None, side, Handle(side.cuda_stream)):
+        torch.cuda._sleep(HELD // 10)
+        rows = B.gnnpre_embedding_lookup(table, ids, stream=stream)
+        grad = B.gnnpre_lc_first_layer_grad([table], batch, dY, stream=stream)
+        update = B.gnnpre_orthogonalize(G, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(rows, table[ids]) and np.array_equal(wide(grad), wide(dY)[0].T @ wide(table)[:40])
+        assert torch.equal(update, B.gnnpre_orthogonalize(G))

@@ -49,6 +49,7 @@ def world(monkeypatch):
         return f
 
     monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: {current.cuda_stream: current, side.cuda_stream: side}[handle])
     monkeypatch.setattr(torch.cuda, "current_stream", lambda: current)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)  # (what get_device says of a host tensor)
     monkeypatch.setattr(torch.Tensor, "is_cuda", True)
