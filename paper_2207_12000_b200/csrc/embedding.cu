@@ -120,7 +120,8 @@ int launch_lookup(LookupArgs a, int num_sms, cudaStream_t st) {
     const int64_t pieces = std::max<int64_t>(1, a.dim / E);
     a.lanes = 1;
     while (a.lanes < 32 && a.lanes < pieces) a.lanes *= 2;
-    // Four rows per thread hide the latency of the ids and rows when the machine is full of threads anyway; few rows are spread.
+    // Four rows per thread hide the latency of the ids and rows when the machine is full of threads anyway; few rows are spread.  us,
+    // one row / four: 1,000 rows of 602 fp16 2.9 / 3.9, 4,096 of 128 fp32 2.4 / 2.5, 18,944 (the border is at 9,472) 5.3 / 4.0, 400,000 88 / 62.
     const bool few = a.count * a.lanes <= (int64_t)num_sms * 2048;
     const int64_t groups = few ? a.count : (a.count + 3) / 4;
     const int64_t blocks = (groups * a.lanes + kLookupThreads - 1) / kLookupThreads;
@@ -172,14 +173,19 @@ __global__ void k_clear(const Clear c) { clear_share(c, blockIdx.x, gridDim.x); 
 // ------------------------------------------------------------------------------------------------ sorting
 
 constexpr int kOneCtaPerThread = 8;
-constexpr int kOneCtaKeys = 1024 * kOneCtaPerThread;  // by a CTA of 1024 threads, fewer keys by one of 512 or 256
+// By a CTA of 1024 threads, fewer keys by one of 512 or 256.  us a gradient, one CTA / blocks of keys: 500 ids into 1,000 rows 9.8 / 12.7,
+// into 169,343 13.4 / 21.1; 3,000 ids 15.7 / 16.0 and 18.4 / 24.1; 5,000 18.8 / 16.8 and 24.2 / 26.5; 8,192, where shared memory ends,
+// 22.7 / 17.4 and 29.7 / 26.9: keys of one digit would pay from some 3,000 on, those of two from 6,000.
+constexpr int kOneCtaKeys = 1024 * kOneCtaPerThread;
 constexpr int kOneCtaDigit = 8;                  // bits
 constexpr int kSortThreads = 512;
 // Keys of a block: 2048 (four per thread) while such blocks fit the machine at once, two to an SM, else 4096.  The time of a block is
 // that of its threads' rounds.  us a gradient, 4096 / 2048: 65,553 rows 71 / 63, 300,000 62 / 56, 2.4 M 333 / 342.
 constexpr int kSortFew = 4, kSortMany = 8;
 constexpr int kMaxDigit = 11;
-constexpr int kSelfScanBlocks = 64;              // up to here a block adds up the other blocks' counts itself
+// Up to here a block adds up the other blocks' counts itself.  us a gradient into 169,343 rows, so / by a kernel of its own: 20,000 ids (10
+// blocks) 27.6 / 29.3, 65,553 (33) 31.9 / 33.2, 131,072 (64) 39.5 / 38.9, 260,000 (127) 71 / 55.
+constexpr int kSelfScanBlocks = 64;
 
 // Places of one warp's keys among those with the same digit before them in this warp; `counts` is the warp's row of counters.
 // Rounds of 32 neighbouring keys, so the order is kept.  Lanes with the same digit are found bit by bit: the ballots of a round do
@@ -610,7 +616,9 @@ __global__ void __launch_bounds__(kSumThreads) k_table_sums(const SumArgs a) {
 }
 
 constexpr int kJoinThreads = 1024;
-constexpr int kJoinAlone = 32;  // parts that one warp adds up by itself
+// Parts that one warp adds up by itself.  us a gradient with 4 / 32 / 256 / any number: 65,553 ids into 1,000 rows 26 / 23 / 35 / 47, 2.4 M into
+// 65,536 337 / 333 / 347 / 446, 100,000 of one id 45 / 45 / 45 / 391.
+constexpr int kJoinAlone = 32;
 
 // A warp per segment: where a row begins in it that goes on in later ones, their parts are added up.  Rows of more than kJoinAlone
 // parts get the whole CTA: each warp a chain, the chains in their order.
